@@ -164,6 +164,105 @@ pp_status prunepath_ffn_prefill(pp_layer *L, const uint16_t *x, int32_t T, float
                                 const float *inv_temp, float *y, int32_t *expert_idx,
                                 int32_t *count, void *hip_stream);
 
+/* Routing to a fixed number of experts ---------------------------------------
+ * The rule beside the cumulative-mass budget: every token takes its k best
+ * experts, by scores that a balance bias and groups of experts may steer.
+ *   z = g with +inf counted as the largest float; an expert whose logit or
+ *       selection bias is -inf or NaN takes no part for that token
+ *   s = softmax(z) over the row (PP_SCORE_SOFTMAX) or sigmoid(z)
+ *       (PP_SCORE_SIGMOID)
+ *   c = s + sel_bias, or the order of z when sel_bias is NULL.  The bias acts
+ *       on the choice alone, never on a weight.
+ *   The E experts are n_groups groups of E / n_groups consecutive ones.  A
+ *       group is worth its largest c, or with PP_GROUP_TOP2 the sum of its two
+ *       largest c (of s when sel_bias is NULL; of one expert, that one's); the
+ *       top_groups best groups that hold an expert stay.
+ *   chosen: the k largest c of the groups that stay; equal ones, of groups
+ *       too, by ascending index.  c is compared in 64 bits.
+ *   w_j = scale s_j, or with PP_TOPK_RENORM scale s_j / (sum of the chosen s).
+ * Arguments shared by the calls below:
+ *   k          : experts per token, 1 .. top_groups * (E / n_groups)
+ *   n_groups   : divides E; 1 .. 16 (PP_EUNSUPPORTED above)
+ *   top_groups : 1 .. n_groups (n_groups 1, top_groups 1: no groups)
+ *   sel_bias   : [E] fp32 or NULL
+ *   scale      : finite factor of every weight
+ *   flags      : PP_SCORE_* | PP_TOPK_RENORM | PP_GROUP_TOP2
+ *   expert_idx : [T, k] int32; row t holds the chosen experts in descending
+ *                order of c, then -1 where fewer than k can be chosen
+ *   gate_w     : [T, k] fp32, the weights of the same slots, 0 in empty ones
+ * Results do not depend on T or on the other tokens.  Nothing is allocated
+ * and nothing but the outputs (and the handle's router scratch) is written, so
+ * the calls may be captured; those without a handle may run at the same time
+ * as any other. */
+#define PP_SCORE_SOFTMAX 0u
+#define PP_SCORE_SIGMOID 1u
+#define PP_TOPK_RENORM 2u
+#define PP_GROUP_TOP2 4u
+/* prunepath_route_topk_grad only: dg += the gradient instead of dg = */
+#define PP_GRAD_ADD 8u
+
+/* prunepath_route_topk -- the rule above on the logits of a handle's router,
+ * g = (W_r x + b) * inv_temp[t], the ones that prunepath_route selects on.
+ *   x, T, inv_temp : as for prunepath_route
+ *   logits         : [T, E] fp32 out or NULL (what prunepath_router_loss and
+ *                    prunepath_route_topk_grad take as g)
+ * PP_EINVAL: NULL L, x, expert_idx or gate_w; T, k, n_groups, top_groups, scale
+ * or flags outside the above; an fp32 or int32 array not 4-byte aligned. */
+pp_status prunepath_route_topk(pp_layer *L, const uint16_t *x, int32_t T, const float *inv_temp,
+                               int32_t k, int32_t n_groups, int32_t top_groups,
+                               const float *sel_bias, float scale, uint32_t flags,
+                               int32_t *expert_idx, float *gate_w, float *logits,
+                               void *hip_stream);
+
+/* prunepath_route_topk_logits -- the rule on logits g [T, E] fp32 that the
+ * caller has.  Needs no handle.  1 <= T <= 2^22, 1 <= E <= 256. */
+pp_status prunepath_route_topk_logits(const float *g, int32_t T, int32_t E, int32_t k,
+                                      int32_t n_groups, int32_t top_groups,
+                                      const float *sel_bias, float scale, uint32_t flags,
+                                      int32_t *expert_idx, float *gate_w, void *hip_stream);
+
+/* prunepath_route_topk_grad -- dL/dg from dL/dgate_w, the choice held fixed:
+ * with a_j = dgate_w_j of the slots that name an expert and q_j = w_j / scale
+ *   softmax               dg_e = scale p_e ([e chosen] a_e - sum_j p_j a_j)
+ *   sigmoid               dg_e = scale s_e (1 - s_e) a_e
+ *   renormalised softmax  dg_e = scale q_e (a_e - sum_j q_j a_j)
+ *   renormalised sigmoid  dg_e = scale q_e (1 - s_e) (a_e - sum_j q_j a_j)
+ * and 0 for every other expert.  All of dg [T, E] is written; with PP_GRAD_ADD
+ * the gradient is added to what dg holds (that of prunepath_router_loss, say).
+ *   g, expert_idx : the forward call's logits and choice (a slot outside
+ *                   0 .. E - 1, or one whose logit takes no part, is empty;
+ *                   slots that name one expert add up); 1 <= k <= E
+ *   dgate_w       : [T, k] fp32; entries of empty slots are not read as
+ *                   numbers (they may be NaN)
+ *   flags         : the forward call's, and PP_GRAD_ADD
+ * dg may alias no other array.  The selection bias gets no gradient. */
+pp_status prunepath_route_topk_grad(const float *g, int32_t T, int32_t E, int32_t k,
+                                    const int32_t *expert_idx, const float *dgate_w, float scale,
+                                    uint32_t flags, float *dg, void *hip_stream);
+
+/* prunepath_ffn_decode_routed, prunepath_ffn_prefill_routed -- the experts'
+ * products on a choice that the caller gives (that of prunepath_route_topk, or
+ * of any router):
+ *   y_t = sum_j gate_w[t, j] FFN_{expert_idx[t, j]}(x_t)   (+ b_proj)
+ *   x          : [T, d] bf16, 1 <= T <= max_tokens
+ *   expert_idx : [T, k] int32, 1 <= k <= E; a slot outside 0 .. E - 1 is empty
+ *                (a token of empty slots alone gets y row 0, or b_proj); an
+ *                expert that a token names twice counts with the sum of its
+ *                weights
+ *   gate_w     : [T, k] fp32 or NULL (weights 1); any values.  They scale the
+ *                experts' hidden values, as PP_AGG_SIGMOID's gates do; the
+ *                handle's own rule and aggregation play no part
+ *   y          : [T, d] fp32 out, overwritten
+ * Decode is for small batches (slices of 64 tokens), prefill for long ones, as
+ * with prunepath_ffn_decode and prunepath_ffn_prefill, whose summation orders
+ * and conditions on the handle they share. */
+pp_status prunepath_ffn_decode_routed(pp_layer *L, const uint16_t *x, int32_t T, int32_t k,
+                                      const int32_t *expert_idx, const float *gate_w, float *y,
+                                      void *hip_stream);
+pp_status prunepath_ffn_prefill_routed(pp_layer *L, const uint16_t *x, int32_t T, int32_t k,
+                                       const int32_t *expert_idx, const float *gate_w, float *y,
+                                       void *hip_stream);
+
 /* prunepath_residual_rmsnorm -- the wiring between stacked FFN layers (not
  * part of the paper's method; its stacked-layer decode workload chains layers
  * with pre-norm residuals, x_{l+1} = x_l + FFN_l(u_l), u_l = RMSNorm(x_l)):
@@ -178,6 +277,50 @@ pp_status prunepath_ffn_prefill(pp_layer *L, const uint16_t *x, int32_t T, float
  * 16-byte aligned or u not 8-byte aligned. */
 pp_status prunepath_residual_rmsnorm(const float *x, const float *y, float *x_out, int32_t T,
                                      int32_t d, float eps, uint16_t *u, void *hip_stream);
+
+/* prunepath_residual_layernorm -- residual add and layer norm, the wiring of
+ * GELU-MLP blocks (prunepath_create_mlp):
+ *   r = x + y  (y NULL: r = x),  mu = mean_j r,  v = mean_j (r - mu)^2,
+ *   rstd = 1 / sqrt(v + eps),  u = (r - mu) rstd w + b
+ *   x, y  : [T, d] fp32
+ *   x_out : [T, d] fp32 out, r; NULL: not written.  May be x or y.
+ *   w, b  : [d] fp32, or NULL (1 and 0)
+ *   u     : [T, d] out, bf16 (rounded to nearest even once, at the end), or
+ *           fp32 with PP_NORM_F32.  Aliases no other array.
+ *   stats : [T, 2] fp32 out, (mu, rstd) of each row for the gradient, or NULL
+ * Any 1 <= d <= 65536, 1 <= T <= 2^20.  Sums are fp32 in an order that does not
+ * depend on T (it does on d and on whether every array is 16-byte aligned, u
+ * and du of bf16 8-byte, which the fastest path needs).
+ * PP_EINVAL: NULL x or u; sizes outside the above; eps negative, NaN or
+ * infinite; unknown flags; an array not aligned to its elements; u equal to x,
+ * y or x_out. */
+#define PP_NORM_F32 1u
+pp_status prunepath_residual_layernorm(const float *x, const float *y, float *x_out, int32_t T,
+                                       int32_t d, float eps, const float *w, const float *b,
+                                       void *u, float *stats, uint32_t flags, void *hip_stream);
+
+/* prunepath_residual_layernorm_grad -- its gradient.  With a = w du and
+ * hat = (r - mu) rstd:
+ *   dx = dres + rstd (a - mean_j a - hat mean_j (a hat))
+ *   dw = sum_t du hat,   db = sum_t du
+ * dx is dL/dx and dL/dy alike (r = x + y).
+ *   x_out : [T, d] fp32, the forward call's r;  stats: its (mu, rstd)
+ *   du    : [T, d], bf16, or fp32 with PP_NORM_F32
+ *   dres  : [T, d] fp32, the gradient that reaches r past the norm, or NULL
+ *   dx    : [T, d] fp32 out; may be dres, no other input
+ *   dw, db: [d] fp32 out, either or both NULL
+ *   workspace : prunepath_residual_layernorm_grad_workspace(T, d) bytes, 4-byte
+ *               aligned (16 for the fastest path), no initial contents needed;
+ *               may be NULL when dw and db are.  Calls that can overlap need
+ *               one each, two captured graphs among them.
+ * Repeated calls give identical bits: the order of every sum is fixed by
+ * (T, d) and the arrays' alignment.
+ * PP_EINVAL: NULL x_out, du, stats or dx; the rest as for the forward call. */
+size_t prunepath_residual_layernorm_grad_workspace(int32_t T, int32_t d); /* 0 for bad sizes */
+pp_status prunepath_residual_layernorm_grad(const float *x_out, const void *du, const float *dres,
+                                            int32_t T, int32_t d, const float *w,
+                                            const float *stats, float *dx, float *dw, float *db,
+                                            void *workspace, uint32_t flags, void *hip_stream);
 
 /* prunepath_router_loss -- the routing regularisers of the training
  * objective and their gradient, over a batch of B router-logit rows

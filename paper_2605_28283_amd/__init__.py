@@ -12,6 +12,11 @@ from ._lib import (EXPORTED, PP_AGG_SIGMOID, PP_AGG_SUM, PP_EHIP, PP_EINVAL, PP_
                    prunepath_create_mlp,
                    prunepath_destroy, prunepath_ffn_decode, prunepath_ffn_prefill,
                    prunepath_profile_begin, prunepath_profile_end, prunepath_residual_rmsnorm,
+                   PP_GRAD_ADD, PP_GROUP_TOP2, PP_NORM_F32, PP_SCORE_SIGMOID, PP_SCORE_SOFTMAX,
+                   PP_TOPK_RENORM, prunepath_ffn_decode_routed, prunepath_ffn_prefill_routed,
+                   prunepath_residual_layernorm, prunepath_residual_layernorm_grad,
+                   prunepath_residual_layernorm_grad_workspace, prunepath_route_topk,
+                   prunepath_route_topk_grad, prunepath_route_topk_logits,
                    prunepath_route, prunepath_router_loss, prunepath_router_loss_noalloc,
                    prunepath_router_loss_workspace,
                    prunepath_status_string)

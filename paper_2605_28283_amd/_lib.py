@@ -27,6 +27,13 @@ PP_SELECT_LTE = 8
 PP_AGG_SUM = 0
 PP_AGG_SIGMOID = 2
 
+PP_SCORE_SOFTMAX = 0
+PP_SCORE_SIGMOID = 1
+PP_TOPK_RENORM = 2
+PP_GROUP_TOP2 = 4
+PP_GRAD_ADD = 8
+PP_NORM_F32 = 1
+
 PP_KERNEL_ROUTE = 0
 PP_KERNEL_DISPATCH = 1
 PP_KERNEL_GATEUP = 2
@@ -38,6 +45,10 @@ EXPORTED = ("prunepath_create", "prunepath_create_mlp", "prunepath_route", "prun
             "prunepath_profile_begin", "prunepath_profile_end", "prunepath_residual_rmsnorm",
             "prunepath_router_loss_workspace", "prunepath_router_loss",
             "prunepath_router_loss_noalloc",
+            "prunepath_route_topk", "prunepath_route_topk_logits", "prunepath_route_topk_grad",
+            "prunepath_ffn_decode_routed", "prunepath_ffn_prefill_routed",
+            "prunepath_residual_layernorm", "prunepath_residual_layernorm_grad_workspace",
+            "prunepath_residual_layernorm_grad",
             "prunepath_kmeans_workspace", "prunepath_balanced_kmeans")
 
 
@@ -93,6 +104,22 @@ def load():
         lib.prunepath_router_loss.restype = ctypes.c_int
         lib.prunepath_router_loss_noalloc.argtypes = [P, I32, I32, F32, F32, F32, F32, P, P, P]
         lib.prunepath_router_loss_noalloc.restype = ctypes.c_int
+        lib.prunepath_route_topk.argtypes = [P, P, I32, P, I32, I32, I32, P, F32, U32, P, P, P, P]
+        lib.prunepath_route_topk_logits.argtypes = [P, I32, I32, I32, I32, I32, P, F32, U32, P, P,
+                                                    P]
+        lib.prunepath_route_topk_grad.argtypes = [P, I32, I32, I32, P, P, F32, U32, P, P]
+        lib.prunepath_ffn_decode_routed.argtypes = [P, P, I32, I32, P, P, P, P]
+        lib.prunepath_ffn_prefill_routed.argtypes = [P, P, I32, I32, P, P, P, P]
+        lib.prunepath_residual_layernorm.argtypes = [P, P, P, I32, I32, F32, P, P, P, P, U32, P]
+        lib.prunepath_residual_layernorm_grad_workspace.argtypes = [I32, I32]
+        lib.prunepath_residual_layernorm_grad_workspace.restype = ctypes.c_size_t
+        lib.prunepath_residual_layernorm_grad.argtypes = [P, P, P, I32, I32, P, P, P, P, P, P, U32,
+                                                          P]
+        for f in (lib.prunepath_route_topk, lib.prunepath_route_topk_logits,
+                  lib.prunepath_route_topk_grad, lib.prunepath_ffn_decode_routed,
+                  lib.prunepath_ffn_prefill_routed, lib.prunepath_residual_layernorm,
+                  lib.prunepath_residual_layernorm_grad):
+            f.restype = ctypes.c_int
         lib.prunepath_kmeans_workspace.argtypes = [I32, I32, I32]
         lib.prunepath_kmeans_workspace.restype = ctypes.c_size_t
         lib.prunepath_balanced_kmeans.argtypes = [P, I32, I32, I32, P, I32, P, P, P, P, P, P, P,
@@ -132,6 +159,23 @@ def _ptr(a, kind=None):
     if want is not None and a.dtype not in want:
         raise TypeError("expected %s array, got %s" % (kind, a.dtype))
     return a.data_ptr()
+
+
+def _here(*arrays):
+    """Tensors on another device than the current one are refused: the kernels
+    run on the current device's stream."""
+    import torch
+    for a in arrays:
+        if a is not None and not isinstance(a, int) and a.is_cuda \
+                and a.device.index != torch.cuda.current_device():
+            raise ValueError("array argument on %s, current device is cuda:%d"
+                             % (a.device, torch.cuda.current_device()))
+
+
+def _size(a, n, name):
+    """A tensor of fewer elements than the call touches is refused."""
+    if a is not None and not isinstance(a, int) and a.numel() < n:
+        raise ValueError("%s: %d elements, the call needs %d" % (name, a.numel(), n))
 
 
 def _stream(stream):
@@ -203,6 +247,105 @@ def prunepath_residual_rmsnorm(x, y, x_out, T, d, eps, u=None, stream=None):
     st = load().prunepath_residual_rmsnorm(_ptr(x, "f32"), _ptr(y, "f32"), _ptr(x_out, "f32"),
                                            T, d, eps, _ptr(u, "bf16"), _stream(stream))
     _check(st, "prunepath_residual_rmsnorm")
+
+
+def prunepath_route_topk(handle, x, T, inv_temp, k, n_groups, top_groups, sel_bias, scale, flags,
+                         expert_idx, gate_w, logits=None, stream=None):
+    """k experts per token by the handle's router (include/prunepath.h has the rule)."""
+    _here(x, inv_temp, sel_bias, expert_idx, gate_w, logits)
+    _size(inv_temp, T, "inv_temp")
+    _size(expert_idx, T * k, "expert_idx")
+    _size(gate_w, T * k, "gate_w")
+    st = load().prunepath_route_topk(handle, _ptr(x, "bf16"), T, _ptr(inv_temp, "f32"), k,
+                                     n_groups, top_groups, _ptr(sel_bias, "f32"), scale, flags,
+                                     _ptr(expert_idx, "i32"), _ptr(gate_w, "f32"),
+                                     _ptr(logits, "f32"), _stream(stream))
+    _check(st, "prunepath_route_topk")
+
+
+def prunepath_route_topk_logits(g, T, E, k, n_groups, top_groups, sel_bias, scale, flags,
+                                expert_idx, gate_w, stream=None):
+    """k experts per row of the logits g [T, E]."""
+    _here(g, sel_bias, expert_idx, gate_w)
+    _size(g, T * E, "g")
+    _size(sel_bias, E, "sel_bias")
+    _size(expert_idx, T * k, "expert_idx")
+    _size(gate_w, T * k, "gate_w")
+    st = load().prunepath_route_topk_logits(_ptr(g, "f32"), T, E, k, n_groups, top_groups,
+                                            _ptr(sel_bias, "f32"), scale, flags,
+                                            _ptr(expert_idx, "i32"), _ptr(gate_w, "f32"),
+                                            _stream(stream))
+    _check(st, "prunepath_route_topk_logits")
+
+
+def prunepath_route_topk_grad(g, T, E, k, expert_idx, dgate_w, scale, flags, dg, stream=None):
+    """dg = dL/dg of the rows' weights (added to dg with PP_GRAD_ADD)."""
+    _here(g, expert_idx, dgate_w, dg)
+    _size(g, T * E, "g")
+    _size(expert_idx, T * k, "expert_idx")
+    _size(dgate_w, T * k, "dgate_w")
+    _size(dg, T * E, "dg")
+    st = load().prunepath_route_topk_grad(_ptr(g, "f32"), T, E, k, _ptr(expert_idx, "i32"),
+                                          _ptr(dgate_w, "f32"), scale, flags, _ptr(dg, "f32"),
+                                          _stream(stream))
+    _check(st, "prunepath_route_topk_grad")
+
+
+def _ffn_routed(name, handle, x, T, k, expert_idx, gate_w, y, stream):
+    _here(x, expert_idx, gate_w, y)
+    _size(expert_idx, T * k, "expert_idx")
+    _size(gate_w, T * k, "gate_w")
+    st = getattr(load(), name)(handle, _ptr(x, "bf16"), T, k, _ptr(expert_idx, "i32"),
+                               _ptr(gate_w, "f32"), _ptr(y, "f32"), _stream(stream))
+    _check(st, name)
+
+
+def prunepath_ffn_decode_routed(handle, x, T, k, expert_idx, gate_w, y, stream=None):
+    """y = the weighted sum of the given experts' outputs (gate_w None: weights 1)."""
+    _ffn_routed("prunepath_ffn_decode_routed", handle, x, T, k, expert_idx, gate_w, y, stream)
+
+
+def prunepath_ffn_prefill_routed(handle, x, T, k, expert_idx, gate_w, y, stream=None):
+    _ffn_routed("prunepath_ffn_prefill_routed", handle, x, T, k, expert_idx, gate_w, y, stream)
+
+
+def prunepath_residual_layernorm(x, y, x_out, T, d, eps, w, b, u, stats=None, flags=0,
+                                 stream=None):
+    """x_out = x + y, u = its layer norm (y, x_out, w, b, stats may be None)."""
+    _here(x, y, x_out, w, b, u, stats)
+    for a, n, name in ((x, T * d, "x"), (y, T * d, "y"), (x_out, T * d, "x_out"), (w, d, "w"),
+                       (b, d, "b"), (u, T * d, "u"), (stats, 2 * T, "stats")):
+        _size(a, n, name)
+    st = load().prunepath_residual_layernorm(_ptr(x, "f32"), _ptr(y, "f32"), _ptr(x_out, "f32"),
+                                             T, d, eps, _ptr(w, "f32"), _ptr(b, "f32"),
+                                             _ptr(u, "f32" if flags & PP_NORM_F32 else "bf16"),
+                                             _ptr(stats, "f32"), flags, _stream(stream))
+    _check(st, "prunepath_residual_layernorm")
+
+
+def prunepath_residual_layernorm_grad_workspace(T, d):
+    """Workspace bytes prunepath_residual_layernorm_grad needs (0 for bad sizes)."""
+    return int(load().prunepath_residual_layernorm_grad_workspace(T, d))
+
+
+def prunepath_residual_layernorm_grad(x_out, du, dres, T, d, w, stats, dx, dw=None, db=None,
+                                      workspace=None, flags=0, stream=None):
+    """dx, and dw and db unless None (then without a workspace if both are)."""
+    _here(x_out, du, dres, w, stats, dx, dw, db, workspace)
+    for a, n, name in ((x_out, T * d, "x_out"), (du, T * d, "du"), (dres, T * d, "dres"),
+                       (w, d, "w"), (stats, 2 * T, "stats"), (dx, T * d, "dx"), (dw, d, "dw"),
+                       (db, d, "db")):
+        _size(a, n, name)
+    if (dw is not None or db is not None) and workspace is not None \
+            and not isinstance(workspace, int):
+        need = prunepath_residual_layernorm_grad_workspace(T, d)
+        if workspace.numel() * workspace.element_size() < need:
+            raise ValueError("workspace: the call needs %d bytes" % need)
+    st = load().prunepath_residual_layernorm_grad(
+        _ptr(x_out, "f32"), _ptr(du, "f32" if flags & PP_NORM_F32 else "bf16"),
+        _ptr(dres, "f32"), T, d, _ptr(w, "f32"), _ptr(stats, "f32"), _ptr(dx, "f32"),
+        _ptr(dw, "f32"), _ptr(db, "f32"), _ptr(workspace), flags, _stream(stream))
+    _check(st, "prunepath_residual_layernorm_grad")
 
 
 def prunepath_router_loss_workspace(B, E):

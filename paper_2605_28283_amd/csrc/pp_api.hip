@@ -108,8 +108,8 @@ pp_status run_ffn(pp_layer *L, const uint16_t *x, int32_t T, float tau, const fl
         hipError_t e = launch_route(L, xs, n, tau, it, idx, cnt, nullptr, !prefill && !fuse, s,
                                     !fuse);
         if (e == hipSuccess)
-            e = prefill ? launch_prefill_ffn(L, xs, n, ys, s)
-                        : launch_decode_ffn(L, xs, n, ys, all_kept && n >= 16, s,
+            e = prefill ? launch_prefill_ffn(L, xs, n, ys, L->flags, s)
+                        : launch_decode_ffn(L, xs, n, ys, all_kept && n >= 16, L->flags, s,
                                             fuse ? &dsel : nullptr);
         if (e != hipSuccess) return hip_status(e);
     }

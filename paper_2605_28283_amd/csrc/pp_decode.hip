@@ -995,8 +995,8 @@ void launch_gateup_dec_t(const GUParams &gp, int T, int num_cu, hipStream_t s) {
 }
 
 hipError_t launch_decode_ffn(pp_layer *L, const uint16_t *x, int T, float *y, bool dense,
-                             hipStream_t s, const DecodeSelect *sel) {
-    GUParams gp = gu_params(L, x, T, false);
+                             uint32_t flags, hipStream_t s, const DecodeSelect *sel) {
+    GUParams gp = gu_params(L, x, T, flags, false);
     if (sel) {
         if (T != 1 || dense) return hipErrorInvalidValue;
         gp.select_here = 1;

@@ -791,7 +791,7 @@ DNParams dn_params(pp_layer *L, int T, float *y) {
 // Gate/up of a decode batch in which every token keeps every expert (dense):
 // the grouped kernel above, its groups from the decode plan.
 void launch_gateup_dense_dec(pp_layer *L, const uint16_t *x, int T, hipStream_t s) {
-    const GUParams gp = gu_params(L, x, T, false);
+    const GUParams gp = gu_params(L, x, T, L->flags, false);
     if (L->gated)
         hipLaunchKernelGGL((gateup_pf_k<true, true>), dim3(L->num_cu), dim3(kGuThreads), 0, s, gp);
     else
@@ -808,7 +808,8 @@ counter_layout counters_for(const pp_dims &dm, int max_tokens) {
     return c;
 }
 
-hipError_t launch_prefill_ffn(pp_layer *L, const uint16_t *x, int T, float *y, hipStream_t s) {
+hipError_t launch_prefill_ffn(pp_layer *L, const uint16_t *x, int T, float *y, uint32_t flags,
+                              hipStream_t s) {
     const pp_dims &dm = L->dm;
     const counter_layout cl = counters_for(dm, L->max_tokens);
     prof_mark(L, PP_KERNEL_DISPATCH, s, true);
@@ -818,7 +819,7 @@ hipError_t launch_prefill_ffn(pp_layer *L, const uint16_t *x, int T, float *y, h
     prof_mark(L, PP_KERNEL_DISPATCH, s, false);
     hipError_t err = hipGetLastError();
     if (err != hipSuccess) return err;
-    const GUParams gp = gu_params(L, x, T, true);
+    const GUParams gp = gu_params(L, x, T, flags, true);
     prof_mark(L, PP_KERNEL_GATEUP, s, true);
     // one workgroup per CU (the kernel's registers and LDS allow no more)
     if (L->gated)

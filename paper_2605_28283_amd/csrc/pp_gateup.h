@@ -358,7 +358,7 @@ int resident(K kernel, int threads) {
     return n;
 }
 
-inline GUParams gu_params(pp_layer *L, const uint16_t *x, int T, bool prefill) {
+inline GUParams gu_params(pp_layer *L, const uint16_t *x, int T, uint32_t flags, bool prefill) {
     const pp_dims &dm = L->dm;
     const counter_layout cl = counters_for(dm, L->max_tokens);
     GUParams P;
@@ -370,7 +370,7 @@ inline GUParams gu_params(pp_layer *L, const uint16_t *x, int T, bool prefill) {
     P.Wgu = L->Wgu;
     P.bfc = L->bfc;
     P.gsig = L->gsig;
-    P.flags = L->flags;
+    P.flags = flags;
     P.plan = plan_view(L, prefill);
     P.emask = L->emask;
     P.abpart = L->abpart;

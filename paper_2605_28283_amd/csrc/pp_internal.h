@@ -131,7 +131,7 @@ struct pp_layer {
     uint32_t *counters; // arrival counters, zero between calls
     size_t n_counters;
     uint32_t *selmask;  // [max_tokens][8] kept-expert bitmask per token
-    float *gsig;        // [max_tokens][E] expert scale (sigmoid(g) or 1)
+    float *gsig;        // [max_tokens][E] expert scale (sigmoid(g), 1 or the caller's weight)
     int32_t *idx_tmp;   // [max_tokens][E] used when the caller passes no expert_idx
     int32_t *cnt_tmp;   // [max_tokens]
     float *abpart;      // [kAbPartRows][256] K-split partial gate/up outputs
@@ -189,10 +189,12 @@ struct DecodeSelect {
     int32_t *idx;
     int32_t *count;
 };
+// flags: the layer's, or PP_AGG_SIGMOID for pairs scaled by gsig.
 hipError_t launch_decode_ffn(pp_layer *L, const uint16_t *x, int T, float *y, bool dense,
-                             hipStream_t s, const DecodeSelect *sel = nullptr);
+                             uint32_t flags, hipStream_t s, const DecodeSelect *sel = nullptr);
 void launch_gateup_dense_dec(pp_layer *L, const uint16_t *x, int T, hipStream_t s);
-hipError_t launch_prefill_ffn(pp_layer *L, const uint16_t *x, int T, float *y, hipStream_t s);
+hipError_t launch_prefill_ffn(pp_layer *L, const uint16_t *x, int T, float *y, uint32_t flags,
+                              hipStream_t s);
 
 inline PlanView plan_view(pp_layer *L, bool prefill) {
     const int G = plan_max_groups(L->dm, L->max_tokens);
