@@ -4,113 +4,437 @@
 //   dx = dres + rstd (a - mean(a) - hat mean(a hat)),  a = w du, hat = (r - mu) rstd
 //   dw = sum_t du hat,  db = sum_t du
 // Not part of the paper's method: the norm of the GELU-MLP blocks whose FFN
-// prunepath_create_mlp makes.  All sums are fp32 in an order fixed by (T, d).
+// prunepath_create_mlp makes.  Bound by memory: each input is read once and
+// each output written once.
+//
+// A row of up to 8192 values stays in registers between its sums and its
+// outputs: one wavefront for up to 1024 (four rows a workgroup, no barrier),
+// four for up to 4096, eight for up to 8192.  Columns are moved four at a
+// time where d and every array allow it, else one at a time.  Longer rows are
+// read again for every sum.
+// The gradient's workgroups walk over rows and keep the column sums of du hat
+// and du in registers; their partial sums (at most kLnBlocks rows of 2 d) are
+// added by a second launch.
+// All sums are fp32, their order fixed by (T, d) and the kind of columns, that
+// of a row's sums by d and that alone; the partial sums are added in fp64.
 #include "pp_internal.h"
 
 namespace pp {
 namespace {
 
 constexpr int kLnThreads = 256;
+constexpr int kLnBlocks = 512;   // gradient workgroups, two to a CU
+constexpr int kLnRegWidth = 8192;
 
-// Sum over the workgroup, the same in every thread.
-__device__ __forceinline__ float block_total(float v, float *ws) {
-    const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6;
-    const float t = lane_value(wave_scan_f32(v), 63);
-    __syncthreads();
-    if (lane == 0) ws[wv] = t;
-    __syncthreads();
-    return (ws[0] + ws[1]) + (ws[2] + ws[3]);
+__device__ __forceinline__ float wave_total(float v) {
+    return lane_value(wave_scan_f32(v), 63);
 }
 
-__device__ __forceinline__ float load_du(const void *p, size_t i, bool f32) {
-    return f32 ? static_cast<const float *>(p)[i]
-               : bf16_to_f32(static_cast<const uint16_t *>(p)[i]);
-}
-
-__global__ __launch_bounds__(kLnThreads) void layernorm_k(const float *x, const float *y,
-                                                          float *x_out, int d, float eps,
-                                                          const float *w, const float *b, void *u,
-                                                          float *stats, int f32) {
-    __shared__ float ws[4];
-    const size_t row = (size_t)blockIdx.x * d;
-    float s = 0.0f;
-    for (int c = threadIdx.x; c < d; c += kLnThreads) s += x[row + c] + (y ? y[row + c] : 0.0f);
-    const float mu = block_total(s, ws) / (float)d;
-    s = 0.0f;
-    for (int c = threadIdx.x; c < d; c += kLnThreads) {
-        const float r = x[row + c] + (y ? y[row + c] : 0.0f);
-        s += (r - mu) * (r - mu);
-    }
-    const float rstd = 1.0f / sqrtf(block_total(s, ws) / (float)d + eps);
-    for (int c = threadIdx.x; c < d; c += kLnThreads) {
-        const float r = x[row + c] + (y ? y[row + c] : 0.0f);
-        if (x_out) x_out[row + c] = r;
-        const float v = (r - mu) * rstd * (w ? w[c] : 1.0f) + (b ? b[c] : 0.0f);
-        if (f32)
-            static_cast<float *>(u)[row + c] = v;
-        else
-            static_cast<uint16_t *>(u)[row + c] = f32_to_bf16(v);
-    }
-    if (stats && threadIdx.x == 0) {
-        stats[2 * blockIdx.x] = mu;
-        stats[2 * blockIdx.x + 1] = rstd;
+// Sums of n values over the WPR wavefronts of a row, the same in every
+// thread.  slot: LDS for WPR * n floats that no earlier reader still needs.
+template <int WPR, int n>
+__device__ __forceinline__ void row_totals(float (&v)[n], float *slot) {
+#pragma unroll
+    for (int i = 0; i < n; ++i) v[i] = wave_total(v[i]);
+    if constexpr (WPR > 1) {
+        const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6;
+        if (lane == 0) {
+#pragma unroll
+            for (int i = 0; i < n; ++i) slot[i * WPR + wv] = v[i];
+        }
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < n; ++i) {
+            float t = slot[i * WPR];
+#pragma unroll
+            for (int w = 1; w < WPR; ++w) t += slot[i * WPR + w];
+            v[i] = t;
+        }
     }
 }
 
-__global__ __launch_bounds__(kLnThreads) void layernorm_dx_k(const float *r, const void *du,
-                                                             const float *dres, int d,
-                                                             const float *w, const float *stats,
-                                                             float *dx, int f32) {
-    __shared__ float ws[4];
-    const size_t row = (size_t)blockIdx.x * d;
-    const float mu = stats[2 * blockIdx.x], rstd = stats[2 * blockIdx.x + 1];
-    float s1 = 0.0f, s2 = 0.0f;
-    for (int c = threadIdx.x; c < d; c += kLnThreads) {
-        const float a = load_du(du, row + c, f32) * (w ? w[c] : 1.0f);
-        s1 += a;
-        s2 += a * ((r[row + c] - mu) * rstd);
+// V consecutive values of a row.
+template <int V>
+struct Cols {
+    float v[V];
+};
+template <int V>
+__device__ __forceinline__ Cols<V> load_f32(const float *p) {
+    Cols<V> c;
+    if constexpr (V == 4) {
+        const float4 f = *reinterpret_cast<const float4 *>(p);
+        c.v[0] = f.x, c.v[1] = f.y, c.v[2] = f.z, c.v[3] = f.w;
+    } else {
+        c.v[0] = *p;
     }
-    const float m1 = block_total(s1, ws) / (float)d, m2 = block_total(s2, ws) / (float)d;
-    for (int c = threadIdx.x; c < d; c += kLnThreads) {
-        const float a = load_du(du, row + c, f32) * (w ? w[c] : 1.0f);
-        const float v = rstd * (a - m1 - (r[row + c] - mu) * rstd * m2);
-        dx[row + c] = dres ? dres[row + c] + v : v;
+    return c;
+}
+template <int V>
+__device__ __forceinline__ void store_f32(float *p, const Cols<V> &c) {
+    if constexpr (V == 4)
+        *reinterpret_cast<float4 *>(p) = make_float4(c.v[0], c.v[1], c.v[2], c.v[3]);
+    else
+        *p = c.v[0];
+}
+// bf16, rounded to nearest even by the hardware (NaN stays NaN).
+__device__ __forceinline__ uint32_t bf16_bits(float f) {
+    return __builtin_bit_cast(uint16_t, static_cast<__bf16>(f));
+}
+template <int V, bool F32>
+__device__ __forceinline__ void store_u(void *u, size_t i, const Cols<V> &c) {
+    if constexpr (F32)
+        store_f32<V>(static_cast<float *>(u) + i, c);
+    else if constexpr (V == 4)
+        *reinterpret_cast<uint2 *>(static_cast<uint16_t *>(u) + i) =
+            make_uint2(bf16_bits(c.v[0]) | (bf16_bits(c.v[1]) << 16),
+                       bf16_bits(c.v[2]) | (bf16_bits(c.v[3]) << 16));
+    else
+        static_cast<uint16_t *>(u)[i] = (uint16_t)bf16_bits(c.v[0]);
+}
+template <int V, bool F32>
+__device__ __forceinline__ Cols<V> load_du(const void *p, size_t i) {
+    if constexpr (F32) return load_f32<V>(static_cast<const float *>(p) + i);
+    Cols<V> c;
+    const uint16_t *q = static_cast<const uint16_t *>(p) + i;
+    if constexpr (V == 4) {
+        const uint2 b = *reinterpret_cast<const uint2 *>(q);
+        c.v[0] = __uint_as_float(b.x << 16), c.v[1] = __uint_as_float(b.x & 0xFFFF0000u);
+        c.v[2] = __uint_as_float(b.y << 16), c.v[3] = __uint_as_float(b.y & 0xFFFF0000u);
+    } else {
+        c.v[0] = bf16_to_f32(*q);
+    }
+    return c;
+}
+
+struct LnParams {
+    const float *x, *y;
+    float *x_out;
+    int T, d;
+    float eps;
+    const float *w, *b;
+    void *u;
+    float *stats;
+};
+
+// Columns of V values in a thread's registers: N of them, column i at
+// V (thread + i * 64 WPR); one past the row's end reads the row's last one and
+// counts for nothing.
+template <int WPR, int N, int V, bool F32>
+__global__ __launch_bounds__(WPR == 8 ? 512 : 256) void layernorm_k(LnParams P) {
+    __shared__ float slot[2][WPR];
+    constexpr int kRows = WPR == 1 ? 4 : 1, kTh = 64 * WPR;
+    const int tid = WPR == 1 ? threadIdx.x & 63 : threadIdx.x;
+    const int t = blockIdx.x * kRows + (WPR == 1 ? threadIdx.x >> 6 : 0);
+    if (t >= P.T) return;  // whole wavefronts of a workgroup without barriers
+    const int n = P.d / V;
+    const size_t row = (size_t)t * P.d;
+    int at[N];
+    Cols<V> r[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) at[i] = V * min(tid + i * kTh, n - 1);
+#pragma unroll
+    for (int i = 0; i < N; ++i) r[i] = load_f32<V>(P.x + row + at[i]);
+    if (P.y) {
+        Cols<V> y[N];
+#pragma unroll
+        for (int i = 0; i < N; ++i) y[i] = load_f32<V>(P.y + row + at[i]);
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+#pragma unroll
+            for (int j = 0; j < V; ++j) r[i].v[j] += y[i].v[j];
+    }
+    float s[1] = {0.0f};
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+        if (tid + i * kTh < n) {
+            if (P.x_out) store_f32<V>(P.x_out + row + at[i], r[i]);
+#pragma unroll
+            for (int j = 0; j < V; ++j) s[0] += r[i].v[j];
+        }
+    row_totals<WPR>(s, slot[0]);
+    const float mu = s[0] / (float)P.d;
+    s[0] = 0.0f;
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+            r[i].v[j] -= mu;
+            if (tid + i * kTh < n) s[0] += r[i].v[j] * r[i].v[j];
+        }
+    row_totals<WPR>(s, slot[1]);
+    const float rstd = 1.0f / sqrtf(s[0] / (float)P.d + P.eps);
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        if (tid + i * kTh >= n) continue;
+        Cols<V> w, b;
+#pragma unroll
+        for (int j = 0; j < V; ++j) w.v[j] = 1.0f, b.v[j] = 0.0f;
+        if (P.w) w = load_f32<V>(P.w + at[i]);
+        if (P.b) b = load_f32<V>(P.b + at[i]);
+#pragma unroll
+        for (int j = 0; j < V; ++j) r[i].v[j] = r[i].v[j] * rstd * w.v[j] + b.v[j];
+        store_u<V, F32>(P.u, row + at[i], r[i]);
+    }
+    if (P.stats && tid == 0) {
+        P.stats[2 * (size_t)t] = mu;
+        P.stats[2 * (size_t)t + 1] = rstd;
     }
 }
 
-// Column sums over kLnRows rows at a time: part [nb][2][d].
-constexpr int kLnRows = 64;
-__global__ __launch_bounds__(kLnThreads) void layernorm_dw_k(const float *r, const void *du, int T,
-                                                             int d, const float *stats,
-                                                             float *part, int f32) {
-    const int c = blockIdx.x * kLnThreads + threadIdx.x, t0 = blockIdx.y * kLnRows;
-    if (c >= d) return;
+// Any row, read once for each sum and once for the outputs.
+template <bool F32>
+__global__ __launch_bounds__(kLnThreads) void layernorm_long_k(LnParams P) {
+    __shared__ float slot[2][4];
+    const size_t row = (size_t)blockIdx.x * P.d;
+    float s[1] = {0.0f};
+    for (int c = threadIdx.x; c < P.d; c += kLnThreads)
+        s[0] += P.x[row + c] + (P.y ? P.y[row + c] : 0.0f);
+    row_totals<4>(s, slot[0]);
+    const float mu = s[0] / (float)P.d;
+    s[0] = 0.0f;
+    for (int c = threadIdx.x; c < P.d; c += kLnThreads) {
+        const float v = P.x[row + c] + (P.y ? P.y[row + c] : 0.0f) - mu;
+        s[0] += v * v;
+    }
+    row_totals<4>(s, slot[1]);
+    const float rstd = 1.0f / sqrtf(s[0] / (float)P.d + P.eps);
+    for (int c = threadIdx.x; c < P.d; c += kLnThreads) {
+        const float r = P.x[row + c] + (P.y ? P.y[row + c] : 0.0f);
+        if (P.x_out) P.x_out[row + c] = r;
+        Cols<1> v;
+        v.v[0] = (r - mu) * rstd * (P.w ? P.w[c] : 1.0f) + (P.b ? P.b[c] : 0.0f);
+        store_u<1, F32>(P.u, row + c, v);
+    }
+    if (P.stats && threadIdx.x == 0) {
+        P.stats[2 * (size_t)blockIdx.x] = mu;
+        P.stats[2 * (size_t)blockIdx.x + 1] = rstd;
+    }
+}
+
+// ------------------------------------------------------------------ gradient
+
+struct LnGradParams {
+    const float *r;
+    const void *du;
+    const float *dres;
+    int T, d;
+    const float *w, *stats;
+    float *dx;
+    float *part;  // [workgroups][2][d] column sums of du hat and of du, or NULL
+};
+
+template <int WPR, int N, int V, bool F32>
+__global__ __launch_bounds__(WPR == 8 ? 512 : 256) void layernorm_grad_k(LnGradParams P) {
+    constexpr int kRows = WPR == 1 ? 4 : 1, kTh = 64 * WPR;
+    __shared__ float slot[2][2 * WPR];
+    __shared__ float join[WPR == 1 ? 3 * 2 * N * V * 64 : 1];
+    const int wv = threadIdx.x >> 6;
+    const int tid = WPR == 1 ? threadIdx.x & 63 : threadIdx.x;
+    const int n = P.d / V;
+    int at[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) at[i] = V * min(tid + i * kTh, n - 1);
+    Cols<V> w[N], sw[N], sb[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+#pragma unroll
+        for (int j = 0; j < V; ++j) w[i].v[j] = 1.0f, sw[i].v[j] = 0.0f, sb[i].v[j] = 0.0f;
+        if (P.w) w[i] = load_f32<V>(P.w + at[i]);
+    }
+    const float inv_d = 1.0f / (float)P.d;
+    int par = 0;
+    for (int t = blockIdx.x * kRows + (WPR == 1 ? wv : 0); t < P.T;
+         t += gridDim.x * kRows, par ^= 1) {
+        const size_t row = (size_t)t * P.d;
+        const float mu = P.stats[2 * (size_t)t], rstd = P.stats[2 * (size_t)t + 1];
+        Cols<V> h[N], g[N], o[N];
+#pragma unroll
+        for (int i = 0; i < N; ++i) h[i] = load_f32<V>(P.r + row + at[i]);
+#pragma unroll
+        for (int i = 0; i < N; ++i) g[i] = load_du<V, F32>(P.du, row + at[i]);
+        if (P.dres) {
+#pragma unroll
+            for (int i = 0; i < N; ++i) o[i] = load_f32<V>(P.dres + row + at[i]);
+        } else {
+#pragma unroll
+            for (int i = 0; i < N; ++i)
+#pragma unroll
+                for (int j = 0; j < V; ++j) o[i].v[j] = 0.0f;
+        }
+        float s[2] = {0.0f, 0.0f};
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const bool in = tid + i * kTh < n;
+#pragma unroll
+            for (int j = 0; j < V; ++j) {
+                h[i].v[j] = (h[i].v[j] - mu) * rstd;
+                sw[i].v[j] += g[i].v[j] * h[i].v[j];
+                sb[i].v[j] += g[i].v[j];
+                g[i].v[j] *= w[i].v[j];
+                if (in) {
+                    s[0] += g[i].v[j];
+                    s[1] += g[i].v[j] * h[i].v[j];
+                }
+            }
+        }
+        // two slots in turn: a row's totals are read before the next row's
+        // barrier, and written again only after it
+        row_totals<WPR>(s, slot[par]);
+        const float m1 = s[0] * inv_d, m2 = s[1] * inv_d;
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            if (tid + i * kTh >= n) continue;
+#pragma unroll
+            for (int j = 0; j < V; ++j) o[i].v[j] += rstd * (g[i].v[j] - m1 - h[i].v[j] * m2);
+            store_f32<V>(P.dx + row + at[i], o[i]);
+        }
+    }
+    if (!P.part) return;
+    if constexpr (WPR == 1) {
+        // the four wavefronts' sums, in order
+        if (wv > 0) {
+#pragma unroll
+            for (int i = 0; i < N; ++i)
+#pragma unroll
+                for (int j = 0; j < V; ++j) {
+                    join[(((wv - 1) * 2 + 0) * N * V + i * V + j) * 64 + tid] = sw[i].v[j];
+                    join[(((wv - 1) * 2 + 1) * N * V + i * V + j) * 64 + tid] = sb[i].v[j];
+                }
+        }
+        __syncthreads();
+        if (wv > 0) return;
+        for (int q = 0; q < 3; ++q) {
+#pragma unroll
+            for (int i = 0; i < N; ++i)
+#pragma unroll
+                for (int j = 0; j < V; ++j) {
+                    sw[i].v[j] += join[((q * 2 + 0) * N * V + i * V + j) * 64 + tid];
+                    sb[i].v[j] += join[((q * 2 + 1) * N * V + i * V + j) * 64 + tid];
+                }
+        }
+    }
+    float *pw = P.part + (size_t)blockIdx.x * 2 * P.d;
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+        if (tid + i * kTh < n) {
+            store_f32<V>(pw + at[i], sw[i]);
+            store_f32<V>(pw + P.d + at[i], sb[i]);
+        }
+}
+
+// Rows past kLnRegWidth values: dx, then the column sums.
+template <bool F32>
+__global__ __launch_bounds__(kLnThreads) void layernorm_dx_long_k(LnGradParams P) {
+    __shared__ float slot[8];
+    const size_t row = (size_t)blockIdx.x * P.d;
+    const float mu = P.stats[2 * (size_t)blockIdx.x], rstd = P.stats[2 * (size_t)blockIdx.x + 1];
+    float s[2] = {0.0f, 0.0f};
+    for (int c = threadIdx.x; c < P.d; c += kLnThreads) {
+        const float a = load_du<1, F32>(P.du, row + c).v[0] * (P.w ? P.w[c] : 1.0f);
+        s[0] += a;
+        s[1] += a * ((P.r[row + c] - mu) * rstd);
+    }
+    row_totals<4>(s, slot);
+    const float m1 = s[0] / (float)P.d, m2 = s[1] / (float)P.d;
+    for (int c = threadIdx.x; c < P.d; c += kLnThreads) {
+        const float a = load_du<1, F32>(P.du, row + c).v[0] * (P.w ? P.w[c] : 1.0f);
+        const float v = rstd * (a - m1 - (P.r[row + c] - mu) * rstd * m2);
+        P.dx[row + c] = P.dres ? P.dres[row + c] + v : v;
+    }
+}
+template <bool F32>
+__global__ __launch_bounds__(kLnThreads) void layernorm_cols_long_k(LnGradParams P) {
+    const int c = blockIdx.x * kLnThreads + threadIdx.x;
+    if (c >= P.d) return;
     float sw = 0.0f, sb = 0.0f;
-    for (int t = t0; t < min(t0 + kLnRows, T); ++t) {
-        const float g = load_du(du, (size_t)t * d + c, f32);
-        sw += g * ((r[(size_t)t * d + c] - stats[2 * t]) * stats[2 * t + 1]);
+    for (int t = blockIdx.y; t < P.T; t += gridDim.y) {
+        const size_t i = (size_t)t * P.d + c;
+        const float g = load_du<1, F32>(P.du, i).v[0];
+        sw += g * ((P.r[i] - P.stats[2 * (size_t)t]) * P.stats[2 * (size_t)t + 1]);
         sb += g;
     }
-    part[((size_t)blockIdx.y * 2) * d + c] = sw;
-    part[((size_t)blockIdx.y * 2 + 1) * d + c] = sb;
+    float *pw = P.part + (size_t)blockIdx.y * 2 * P.d;
+    pw[c] = sw;
+    pw[P.d + c] = sb;
 }
 
-__global__ __launch_bounds__(kLnThreads) void layernorm_sum_k(const float *part, int nb, int d,
-                                                              float *dw, float *db) {
-    const int c = blockIdx.x * kLnThreads + threadIdx.x;
-    if (c >= d) return;
-    double sw = 0.0, sb = 0.0;
-    for (int i = 0; i < nb; ++i) {
-        sw += part[((size_t)i * 2) * d + c];
-        sb += part[((size_t)i * 2 + 1) * d + c];
+// dw and db from the nb partial rows of 2 d: 64 columns a workgroup, row
+// i of the partial sums with wavefront i % 16.
+__global__ __launch_bounds__(1024) void layernorm_sum_k(const float *__restrict__ part, int nb,
+                                                        int d, float *__restrict__ dw,
+                                                        float *__restrict__ db) {
+    __shared__ double sum[16][64];
+    const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6;
+    const int c = blockIdx.x * 64 + lane;
+    constexpr int kLoads = 8;
+    double s = 0.0;
+    for (int i0 = wv; i0 < nb; i0 += 16 * kLoads) {
+        float v[kLoads];
+#pragma unroll
+        for (int q = 0; q < kLoads; ++q)
+            v[q] = part[(size_t)min(i0 + 16 * q, nb - 1) * 2 * d + min(c, 2 * d - 1)];
+#pragma unroll
+        for (int q = 0; q < kLoads; ++q) s += i0 + 16 * q < nb ? (double)v[q] : 0.0;
     }
-    if (dw) dw[c] = (float)sw;
-    if (db) db[c] = (float)sb;
+    sum[wv][lane] = s;
+    __syncthreads();
+    if (wv > 0 || c >= 2 * d) return;
+#pragma unroll
+    for (int w = 1; w < 16; ++w) s += sum[w][lane];
+    float *out = c < d ? dw : db;
+    if (out) out[c < d ? c : c - d] = (float)s;
 }
 
 constexpr int kLnMaxRows = 1 << 20, kLnMaxWidth = 1 << 16;
 
-inline int ln_blocks(int T) { return (T + kLnRows - 1) / kLnRows; }
+// Gradient workgroups (and partial rows): one for each four rows or each row,
+// up to kLnBlocks.
+inline int ln_blocks(int T, int d) {
+    const int rows = d <= 1024 ? 4 : 1, n = (T + rows - 1) / rows;
+    return n < kLnBlocks ? n : kLnBlocks;
+}
+
+template <int WPR, int N, int V, bool F32>
+void launch_ln(const LnParams &P, hipStream_t s) {
+    const int rows = WPR == 1 ? 4 : 1;
+    hipLaunchKernelGGL((layernorm_k<WPR, N, V, F32>), dim3((P.T + rows - 1) / rows),
+                       dim3(WPR == 8 ? 512 : 256), 0, s, P);
+}
+template <int WPR, int N, int V, bool F32>
+void launch_ln(const LnGradParams &P, hipStream_t s) {
+    hipLaunchKernelGGL((layernorm_grad_k<WPR, N, V, F32>), dim3(ln_blocks(P.T, P.d)),
+                       dim3(WPR == 8 ? 512 : 256), 0, s, P);
+}
+
+// The build for a row of d values: V = 4 needs d and every array in whole
+// float4 (u and du of bf16: 8 bytes).
+template <int V, bool F32, typename Params>
+void launch_ln_width(const Params &P, hipStream_t s) {
+    constexpr int q = 4 / V;  // registers' columns per float4
+    if (P.d <= 256)
+        launch_ln<1, 1 * q, V, F32>(P, s);
+    else if (P.d <= 512)
+        launch_ln<1, 2 * q, V, F32>(P, s);
+    else if (P.d <= 1024)
+        launch_ln<1, 4 * q, V, F32>(P, s);
+    else if (P.d <= 2048)
+        launch_ln<4, 2 * q, V, F32>(P, s);
+    else if (P.d <= 4096)
+        launch_ln<4, 4 * q, V, F32>(P, s);
+    else
+        launch_ln<8, 4 * q, V, F32>(P, s);
+}
+template <typename Params>
+void launch_ln_reg(const Params &P, bool vec, bool f32, hipStream_t s) {
+    if (vec)
+        f32 ? launch_ln_width<4, true>(P, s) : launch_ln_width<4, false>(P, s);
+    else
+        f32 ? launch_ln_width<1, true>(P, s) : launch_ln_width<1, false>(P, s);
+}
+
+inline bool whole_vectors(int d, uintptr_t arrays, const void *half, bool f32) {
+    return d % 4 == 0 && arrays % 16 == 0 && (uintptr_t)half % (f32 ? 16 : 8) == 0;
+}
 
 }  // namespace
 }  // namespace pp
@@ -130,15 +454,21 @@ extern "C" pp_status prunepath_residual_layernorm(const float *x, const float *y
           (uintptr_t)stats) & 3) || ((uintptr_t)u & (f32 ? 3 : 1)))
         return PP_EINVAL;
     if (u == (const void *)x || u == (const void *)y || u == (const void *)x_out) return PP_EINVAL;
-    hipLaunchKernelGGL(layernorm_k, dim3(T), dim3(kLnThreads), 0,
-                       static_cast<hipStream_t>(hip_stream), x, y, x_out, d, eps, w, b, u, stats,
-                       (int)f32);
+    hipStream_t s = static_cast<hipStream_t>(hip_stream);
+    const LnParams P = {x, y, x_out, T, d, eps, w, b, u, stats};
+    if (d <= kLnRegWidth)
+        launch_ln_reg(P, whole_vectors(d, (uintptr_t)x | (uintptr_t)y | (uintptr_t)x_out |
+                                              (uintptr_t)w | (uintptr_t)b, u, f32), f32, s);
+    else if (f32)
+        hipLaunchKernelGGL(layernorm_long_k<true>, dim3(T), dim3(kLnThreads), 0, s, P);
+    else
+        hipLaunchKernelGGL(layernorm_long_k<false>, dim3(T), dim3(kLnThreads), 0, s, P);
     return hipGetLastError() == hipSuccess ? PP_OK : PP_EHIP;
 }
 
 extern "C" size_t prunepath_residual_layernorm_grad_workspace(int32_t T, int32_t d) {
     if (T < 1 || T > kLnMaxRows || d < 1 || d > kLnMaxWidth) return 0;
-    return sizeof(float) * 2 * (size_t)ln_blocks(T) * (size_t)d;
+    return sizeof(float) * 2 * (size_t)ln_blocks(T, d) * (size_t)d;
 }
 
 extern "C" pp_status prunepath_residual_layernorm_grad(const float *x_out, const void *du,
@@ -158,14 +488,26 @@ extern "C" pp_status prunepath_residual_layernorm_grad(const float *x_out, const
         return PP_EINVAL;
     if ((const void *)dx == du || dx == x_out || (dw && dw == db)) return PP_EINVAL;
     hipStream_t s = static_cast<hipStream_t>(hip_stream);
-    float *part = static_cast<float *>(workspace);
-    if (dw || db) {
-        const int nb = ln_blocks(T), nc = (d + kLnThreads - 1) / kLnThreads;
-        hipLaunchKernelGGL(layernorm_dw_k, dim3(nc, nb), dim3(kLnThreads), 0, s, x_out, du, T, d,
-                           stats, part, (int)f32);
-        hipLaunchKernelGGL(layernorm_sum_k, dim3(nc), dim3(kLnThreads), 0, s, part, nb, d, dw, db);
+    float *part = dw || db ? static_cast<float *>(workspace) : nullptr;
+    const LnGradParams P = {x_out, du, dres, T, d, w, stats, dx, part};
+    const int nb = ln_blocks(T, d);
+    if (d <= kLnRegWidth) {
+        launch_ln_reg(P, whole_vectors(d, (uintptr_t)x_out | (uintptr_t)dres | (uintptr_t)w |
+                                              (uintptr_t)dx | (uintptr_t)part, du, f32), f32, s);
+    } else {
+        // the column sums first: dx may be dres, which they do not read
+        const dim3 grid((d + kLnThreads - 1) / kLnThreads, nb);
+        if (part && f32)
+            hipLaunchKernelGGL(layernorm_cols_long_k<true>, grid, dim3(kLnThreads), 0, s, P);
+        else if (part)
+            hipLaunchKernelGGL(layernorm_cols_long_k<false>, grid, dim3(kLnThreads), 0, s, P);
+        if (f32)
+            hipLaunchKernelGGL(layernorm_dx_long_k<true>, dim3(T), dim3(kLnThreads), 0, s, P);
+        else
+            hipLaunchKernelGGL(layernorm_dx_long_k<false>, dim3(T), dim3(kLnThreads), 0, s, P);
     }
-    hipLaunchKernelGGL(layernorm_dx_k, dim3(T), dim3(kLnThreads), 0, s, x_out, du, dres, d, w,
-                       stats, dx, (int)f32);
+    if (part)
+        hipLaunchKernelGGL(layernorm_sum_k, dim3((2 * d + 63) / 64), dim3(1024), 0, s, part, nb, d,
+                           dw, db);
     return hipGetLastError() == hipSuccess ? PP_OK : PP_EHIP;
 }
