@@ -138,7 +138,17 @@ def _status_text(s):
         return "unknown"
 
 
-_BF16_LIKE = None
+_KINDS = None
+
+
+def _kinds():
+    """The torch types that an argument of each kind may have."""
+    global _KINDS
+    if _KINDS is None:
+        import torch
+        _KINDS = {"bf16": {torch.bfloat16, torch.int16, torch.uint16}, "f32": {torch.float32},
+                  "i32": {torch.int32}}
+    return _KINDS
 
 
 def _ptr(a, kind=None):
@@ -147,40 +157,43 @@ def _ptr(a, kind=None):
         return None
     if isinstance(a, int):
         return a
-    import torch
-    global _BF16_LIKE
-    if _BF16_LIKE is None:
-        _BF16_LIKE = {torch.bfloat16, torch.int16, torch.uint16}
     if not a.is_cuda:
         raise ValueError("array arguments must live on the GPU")
     if not a.is_contiguous():
         raise ValueError("array arguments must be contiguous")
-    want = {"bf16": _BF16_LIKE, "f32": {torch.float32}, "i32": {torch.int32}}.get(kind)
+    want = _kinds().get(kind)
     if want is not None and a.dtype not in want:
         raise TypeError("expected %s array, got %s" % (kind, a.dtype))
     return a.data_ptr()
 
 
-def _here(*arrays):
-    """Tensors on another device than the current one are refused: the kernels
-    run on the current device's stream."""
+def _arg(a, kind, n, name, dev):
+    """_ptr for the calls that also know how many elements they touch and on
+    which device they run: one pass over a tensor's properties, the reasons
+    only where one does not hold."""
+    if a is None or isinstance(a, int):
+        return a
+    if (a.get_device() == dev and a.is_contiguous() and a.numel() >= n
+            and (kind is None or a.dtype in _kinds()[kind])):
+        return a.data_ptr()
+    _ptr(a, kind)  # raises for anything but the device and the size
+    if a.get_device() != dev:
+        raise ValueError("%s is on %s, the current device is cuda:%d" % (name, a.device, dev))
+    raise ValueError("%s: %d elements, the call needs %d" % (name, a.numel(), n))
+
+
+def _device():
+    """The current device's index."""
     import torch
-    for a in arrays:
-        if a is not None and not isinstance(a, int) and a.is_cuda \
-                and a.device.index != torch.cuda.current_device():
-            raise ValueError("array argument on %s, current device is cuda:%d"
-                             % (a.device, torch.cuda.current_device()))
-
-
-def _size(a, n, name):
-    """A tensor of fewer elements than the call touches is refused."""
-    if a is not None and not isinstance(a, int) and a.numel() < n:
-        raise ValueError("%s: %d elements, the call needs %d" % (name, a.numel(), n))
+    return torch.cuda.current_device()
 
 
 def _stream(stream):
     if stream is None:
         import torch
+        raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)  # 0.1 us; the object takes 3
+        if raw is not None:
+            return raw(torch.cuda.current_device())
         return torch.cuda.current_stream().cuda_stream
     if isinstance(stream, int):
         return stream
@@ -252,51 +265,43 @@ def prunepath_residual_rmsnorm(x, y, x_out, T, d, eps, u=None, stream=None):
 def prunepath_route_topk(handle, x, T, inv_temp, k, n_groups, top_groups, sel_bias, scale, flags,
                          expert_idx, gate_w, logits=None, stream=None):
     """k experts per token by the handle's router (include/prunepath.h has the rule)."""
-    _here(x, inv_temp, sel_bias, expert_idx, gate_w, logits)
-    _size(inv_temp, T, "inv_temp")
-    _size(expert_idx, T * k, "expert_idx")
-    _size(gate_w, T * k, "gate_w")
-    st = load().prunepath_route_topk(handle, _ptr(x, "bf16"), T, _ptr(inv_temp, "f32"), k,
-                                     n_groups, top_groups, _ptr(sel_bias, "f32"), scale, flags,
-                                     _ptr(expert_idx, "i32"), _ptr(gate_w, "f32"),
-                                     _ptr(logits, "f32"), _stream(stream))
+    v = _device()
+    st = load().prunepath_route_topk(
+        handle, _arg(x, "bf16", 0, "x", v), T, _arg(inv_temp, "f32", T, "inv_temp", v), k,
+        n_groups, top_groups, _arg(sel_bias, "f32", 0, "sel_bias", v), scale, flags,
+        _arg(expert_idx, "i32", T * k, "expert_idx", v), _arg(gate_w, "f32", T * k, "gate_w", v),
+        _arg(logits, "f32", 0, "logits", v), _stream(stream))
     _check(st, "prunepath_route_topk")
 
 
 def prunepath_route_topk_logits(g, T, E, k, n_groups, top_groups, sel_bias, scale, flags,
                                 expert_idx, gate_w, stream=None):
     """k experts per row of the logits g [T, E]."""
-    _here(g, sel_bias, expert_idx, gate_w)
-    _size(g, T * E, "g")
-    _size(sel_bias, E, "sel_bias")
-    _size(expert_idx, T * k, "expert_idx")
-    _size(gate_w, T * k, "gate_w")
-    st = load().prunepath_route_topk_logits(_ptr(g, "f32"), T, E, k, n_groups, top_groups,
-                                            _ptr(sel_bias, "f32"), scale, flags,
-                                            _ptr(expert_idx, "i32"), _ptr(gate_w, "f32"),
-                                            _stream(stream))
+    v = _device()
+    st = load().prunepath_route_topk_logits(
+        _arg(g, "f32", T * E, "g", v), T, E, k, n_groups, top_groups,
+        _arg(sel_bias, "f32", E, "sel_bias", v), scale, flags,
+        _arg(expert_idx, "i32", T * k, "expert_idx", v), _arg(gate_w, "f32", T * k, "gate_w", v),
+        _stream(stream))
     _check(st, "prunepath_route_topk_logits")
 
 
 def prunepath_route_topk_grad(g, T, E, k, expert_idx, dgate_w, scale, flags, dg, stream=None):
     """dg = dL/dg of the rows' weights (added to dg with PP_GRAD_ADD)."""
-    _here(g, expert_idx, dgate_w, dg)
-    _size(g, T * E, "g")
-    _size(expert_idx, T * k, "expert_idx")
-    _size(dgate_w, T * k, "dgate_w")
-    _size(dg, T * E, "dg")
-    st = load().prunepath_route_topk_grad(_ptr(g, "f32"), T, E, k, _ptr(expert_idx, "i32"),
-                                          _ptr(dgate_w, "f32"), scale, flags, _ptr(dg, "f32"),
-                                          _stream(stream))
+    v = _device()
+    st = load().prunepath_route_topk_grad(
+        _arg(g, "f32", T * E, "g", v), T, E, k, _arg(expert_idx, "i32", T * k, "expert_idx", v),
+        _arg(dgate_w, "f32", T * k, "dgate_w", v), scale, flags, _arg(dg, "f32", T * E, "dg", v),
+        _stream(stream))
     _check(st, "prunepath_route_topk_grad")
 
 
 def _ffn_routed(name, handle, x, T, k, expert_idx, gate_w, y, stream):
-    _here(x, expert_idx, gate_w, y)
-    _size(expert_idx, T * k, "expert_idx")
-    _size(gate_w, T * k, "gate_w")
-    st = getattr(load(), name)(handle, _ptr(x, "bf16"), T, k, _ptr(expert_idx, "i32"),
-                               _ptr(gate_w, "f32"), _ptr(y, "f32"), _stream(stream))
+    v = _device()
+    st = getattr(load(), name)(handle, _arg(x, "bf16", 0, "x", v), T, k,
+                               _arg(expert_idx, "i32", T * k, "expert_idx", v),
+                               _arg(gate_w, "f32", T * k, "gate_w", v), _arg(y, "f32", 0, "y", v),
+                               _stream(stream))
     _check(st, name)
 
 
@@ -306,20 +311,19 @@ def prunepath_ffn_decode_routed(handle, x, T, k, expert_idx, gate_w, y, stream=N
 
 
 def prunepath_ffn_prefill_routed(handle, x, T, k, expert_idx, gate_w, y, stream=None):
+    """The same, organised for long batches."""
     _ffn_routed("prunepath_ffn_prefill_routed", handle, x, T, k, expert_idx, gate_w, y, stream)
 
 
 def prunepath_residual_layernorm(x, y, x_out, T, d, eps, w, b, u, stats=None, flags=0,
                                  stream=None):
     """x_out = x + y, u = its layer norm (y, x_out, w, b, stats may be None)."""
-    _here(x, y, x_out, w, b, u, stats)
-    for a, n, name in ((x, T * d, "x"), (y, T * d, "y"), (x_out, T * d, "x_out"), (w, d, "w"),
-                       (b, d, "b"), (u, T * d, "u"), (stats, 2 * T, "stats")):
-        _size(a, n, name)
-    st = load().prunepath_residual_layernorm(_ptr(x, "f32"), _ptr(y, "f32"), _ptr(x_out, "f32"),
-                                             T, d, eps, _ptr(w, "f32"), _ptr(b, "f32"),
-                                             _ptr(u, "f32" if flags & PP_NORM_F32 else "bf16"),
-                                             _ptr(stats, "f32"), flags, _stream(stream))
+    v, n = _device(), T * d
+    st = load().prunepath_residual_layernorm(
+        _arg(x, "f32", n, "x", v), _arg(y, "f32", n, "y", v), _arg(x_out, "f32", n, "x_out", v),
+        T, d, eps, _arg(w, "f32", d, "w", v), _arg(b, "f32", d, "b", v),
+        _arg(u, "f32" if flags & PP_NORM_F32 else "bf16", n, "u", v),
+        _arg(stats, "f32", 2 * T, "stats", v), flags, _stream(stream))
     _check(st, "prunepath_residual_layernorm")
 
 
@@ -331,20 +335,18 @@ def prunepath_residual_layernorm_grad_workspace(T, d):
 def prunepath_residual_layernorm_grad(x_out, du, dres, T, d, w, stats, dx, dw=None, db=None,
                                       workspace=None, flags=0, stream=None):
     """dx, and dw and db unless None (then without a workspace if both are)."""
-    _here(x_out, du, dres, w, stats, dx, dw, db, workspace)
-    for a, n, name in ((x_out, T * d, "x_out"), (du, T * d, "du"), (dres, T * d, "dres"),
-                       (w, d, "w"), (stats, 2 * T, "stats"), (dx, T * d, "dx"), (dw, d, "dw"),
-                       (db, d, "db")):
-        _size(a, n, name)
-    if (dw is not None or db is not None) and workspace is not None \
-            and not isinstance(workspace, int):
-        need = prunepath_residual_layernorm_grad_workspace(T, d)
+    v, n, lib = _device(), T * d, load()
+    ws = _arg(workspace, None, 0, "workspace", v)
+    if (dw is not None or db is not None) and ws is not workspace:
+        need = lib.prunepath_residual_layernorm_grad_workspace(T, d)
         if workspace.numel() * workspace.element_size() < need:
             raise ValueError("workspace: the call needs %d bytes" % need)
-    st = load().prunepath_residual_layernorm_grad(
-        _ptr(x_out, "f32"), _ptr(du, "f32" if flags & PP_NORM_F32 else "bf16"),
-        _ptr(dres, "f32"), T, d, _ptr(w, "f32"), _ptr(stats, "f32"), _ptr(dx, "f32"),
-        _ptr(dw, "f32"), _ptr(db, "f32"), _ptr(workspace), flags, _stream(stream))
+    st = lib.prunepath_residual_layernorm_grad(
+        _arg(x_out, "f32", n, "x_out", v),
+        _arg(du, "f32" if flags & PP_NORM_F32 else "bf16", n, "du", v),
+        _arg(dres, "f32", n, "dres", v), T, d, _arg(w, "f32", d, "w", v),
+        _arg(stats, "f32", 2 * T, "stats", v), _arg(dx, "f32", n, "dx", v),
+        _arg(dw, "f32", d, "dw", v), _arg(db, "f32", d, "db", v), ws, flags, _stream(stream))
     _check(st, "prunepath_residual_layernorm_grad")
 
 
