@@ -10,17 +10,18 @@
 //   index.  w_j = scale s_j, or scale s_j / (sum of the chosen s).
 //
 // A token takes the 16 lanes of one DPP row, four tokens a wavefront, one
-// wavefront a workgroup.  The four rows of logits are read in whole cache
-// lines into LDS; a lane then holds values of one group only (16 lanes over
-// the next power of two of n_groups), so a group's worth is a reduction in
-// registers and over few lanes.
-// c is formed in 64 bits wherever scores decide (a choice next to a border is
-// that of the definition).  The k passes run on 32-bit keys: the distance from
-// the row's largest c, rounded to a float, its low byte replaced by the
-// expert.  Keys of other distances keep the order of c (both roundings are
-// monotone); where the list has two neighbours of equal upper bits, the first
-// 16 entries are put in order by their c in 64 bits, or, if that many do not
-// hold every entry next to the cut, the row is chosen again from all its c.
+// wavefront a workgroup.  The rows of logits (and the bias) are read in whole
+// cache lines into LDS; a lane then holds values of one group only (16 lanes
+// over the next power of two of n_groups), so a group's worth is a reduction
+// in registers and over few lanes.
+// The k passes run on 32-bit keys: the distance from the row's largest c,
+// rounded to a float, its low byte replaced by the expert, so that one
+// unsigned minimum gives value and index.  Scores are formed in 32 bits for
+// that; a choice that they leave open is made in 64 bits: up to 16 candidates,
+// one a lane, are put in order by their exact c; a row in which that many do
+// not hold everything next to the cut, or two groups are too near, is chosen
+// again from every c in 64 bits by the whole wavefront (choose_row).  So c is
+// compared in 64 bits wherever it matters, and few tokens pay for it.
 // Weights are formed in fp32; renormalised ones from scores relative to the
 // largest chosen one, so a row of scores that all underflow still has them.
 // Deterministic: no floating-point atomics; a token's result does not depend
@@ -60,8 +61,10 @@ struct TopkParams {
     // layout (topk_layout)
     int Gs;          // experts of a group
     int lanes;       // lanes of a group: 16 / (n_groups up to a power of two)
+    int lanes_log;
     int Gp, Rp;      // LDS floats from group to group, from row to row
     uint32_t by_Gs;  // ceil(2^16 / Gs): e / Gs = (e by_Gs) >> 16 for e < 256
+    int pad;         // whether lanes read places without an expert
 };
 
 // NaN and -inf to -inf, +inf to the largest float.
@@ -163,194 +166,330 @@ __device__ __forceinline__ double sigmoid64(float z) {
 __device__ __forceinline__ float rel_sigmoid(float z, float m) {
     return expf(fminf(z, 0.0f) - m) / (1.0f + expf(-fabsf(z)));
 }
+// e^x with the hardware's exponential (1 ulp of a rounded product).
 __device__ __forceinline__ float exp_fast(float x) {
     return __builtin_amdgcn_exp2f(x * 1.44269504088896341f);
 }
+// sigmoid(z) within 4e-7: e = e^-|z| is off by e (|z| 2^-23 + 2^-22) < 2.9e-7
+// (the product with log2 e, the exponential), which counts 1 / (1 + e)^2 of
+// that; 1 + e, its reciprocal and e r add 2^-24 + 2^-23 + 2^-25.
+constexpr float kScoreErr = 6e-7f;
+__device__ __forceinline__ float sigmoid_fast(float z) {
+    const float e = exp_fast(-fabsf(z)), r = __builtin_amdgcn_rcpf(1.0f + e);
+    return z >= 0.0f ? r : e * r;
+}
 
-// NQ: values a lane holds.  SCORES: c is in 64 bits (a bias, or groups worth
-// two scores); else c is the logit.
+// Largest and smallest over the wavefront, sum over it.
+template <typename F>
+__device__ __forceinline__ double wave_reduce(double v, int lane, F f) {
+    auto step = [&](auto st) {
+        constexpr int ST = decltype(st)::value;
+        const unsigned long long u = __builtin_bit_cast(unsigned long long, v);
+        const unsigned long long o =
+            ((unsigned long long)xor_lane<ST>((uint32_t)(u >> 32), lane) << 32) |
+            xor_lane<ST>((uint32_t)u, lane);
+        v = f(v, __builtin_bit_cast(double, o));
+    };
+    step(std::integral_constant<int, 1>{});
+    step(std::integral_constant<int, 2>{});
+    step(std::integral_constant<int, 4>{});
+    step(std::integral_constant<int, 8>{});
+    step(std::integral_constant<int, 16>{});
+    step(std::integral_constant<int, 32>{});
+    return v;
+}
+__device__ __forceinline__ uint32_t wave_min_u32(uint32_t v, int lane) {
+    v = min(v, xor_lane<1>(v, lane));
+    v = min(v, xor_lane<2>(v, lane));
+    v = min(v, xor_lane<4>(v, lane));
+    v = min(v, xor_lane<8>(v, lane));
+    v = min(v, xor_lane<16>(v, lane));
+    return min(v, xor_lane<32>(v, lane));
+}
+
+// e's place in a row in LDS.
+__device__ __forceinline__ int topk_place(const TopkParams &P, int e) {
+    const int g = (int)(__umul24((uint32_t)e, P.by_Gs) >> 16);
+    return g * P.Gp + e - g * P.Gs;
+}
+
+// One row's choice, all of it in 64 bits, by the whole wavefront: lane l has
+// experts l, l + 64, ...  zr, zb: the row and the bias in LDS; zmax: the row's
+// largest logit; worth: 256 doubles of LDS; out: [k].
+__device__ __forceinline__ void choose_row(const TopkParams &P, const float *zr, const float *zb, float zmax,
+                           double *worth, short *out, int lane) {
+    constexpr int NE = kMaxExperts / 64;
+    const bool sig = (P.flags & PP_SCORE_SIGMOID) != 0;
+    const bool top2 = (P.flags & PP_GROUP_TOP2) != 0;
+    double c[NE], s[NE], S = 0.0;
+#pragma unroll
+    for (int q = 0; q < NE; ++q) {
+        const int e = lane + 64 * q;
+        const float z = e < P.E ? zr[topk_place(P, e)] : -INFINITY;
+        c[q] = (double)z;
+        s[q] = 0.0;
+        if (z > -INFINITY) s[q] = sig ? sigmoid64(z) : exp_neg((double)z - (double)zmax);
+        S += s[q];
+    }
+    if (!sig) {
+        S = wave_reduce(S, lane, [](double a, double b) { return a + b; });
+        const double r = S > 0.0 ? rcp64(S) : 0.0;
+#pragma unroll
+        for (int q = 0; q < NE; ++q) s[q] *= r;
+    }
+#pragma unroll
+    for (int q = 0; q < NE; ++q) {
+        const int e = lane + 64 * q;
+        if (P.sel_bias) {
+            const float b = e < P.E ? zb[topk_place(P, e)] : -INFINITY;
+            const double v = s[q] + (double)b;
+            c[q] = c[q] > -INFINITY && b > -INFINITY ? v : -INFINITY;
+        }
+        // without a bias experts are in the order of the logits
+        if (P.n_groups > 1)
+            worth[e] = top2 && !P.sel_bias && c[q] > -INFINITY ? s[q] : c[q];
+    }
+    if (P.n_groups > 1) {
+        __syncthreads();
+        double a = -INFINITY, n = -INFINITY;
+        if (lane < P.n_groups) {
+#pragma unroll 4
+            for (int i = 0; i < P.Gs; ++i) {
+                const double v = worth[lane * P.Gs + i];
+                n = fmax(n, fmin(a, v));
+                a = fmax(a, v);
+            }
+            if (top2 && n > -INFINITY) a += n;
+        }
+        __syncthreads();
+        worth[lane] = a;
+        __syncthreads();
+        int front = 0;
+#pragma unroll 1
+        for (int g = 0; g < P.n_groups; ++g) {
+            const double o = worth[g];
+            front += o > a || (o == a && g < lane) ? 1 : 0;
+        }
+        const unsigned long long stay = __ballot(front < P.top_groups && lane < P.n_groups);
+        __syncthreads();  // worth is free again
+#pragma unroll
+        for (int q = 0; q < NE; ++q) {
+            const int g = (int)(__umul24((uint32_t)(lane + 64 * q), P.by_Gs) >> 16);
+            if (!((stay >> (g & 63)) & 1ull)) c[q] = -INFINITY;
+        }
+    }
+#pragma unroll 1
+    for (int j = 0; j < P.k; ++j) {
+        double best = -INFINITY;
+        uint32_t be = 256u;
+#pragma unroll
+        for (int q = 0; q < NE; ++q) {
+            const bool up = c[q] > best;
+            best = up ? c[q] : best;
+            be = up ? (uint32_t)(lane + 64 * q) : be;
+        }
+        const double top =
+            wave_reduce(best, lane, [](double a, double b) { return fmax(a, b); });
+        const uint32_t e = wave_min_u32(best == top ? be : 256u, lane);
+        if (lane == 0) out[j] = e < 256u ? (short)e : (short)-1;
+#pragma unroll
+        for (int q = 0; q < NE; ++q)
+            if ((uint32_t)(lane + 64 * q) == e) c[q] = -INFINITY;
+    }
+}
+
+// NQ: values a lane holds.  SCORES: scores decide (a bias, or groups worth two
+// scores); else c is the logit and needs no 64 bits.
 template <int NQ, bool SCORES>
 __global__ __launch_bounds__(64) void route_topk_k(TopkParams P) {
-    using C = std::conditional_t<SCORES, double, float>;
-    extern __shared__ float lds[];
-    float *const zs = lds;                                      // [4][Rp]
-    short *const pk = reinterpret_cast<short *>(zs + 4 * P.Rp); // [4][k up to 16s]
+    extern __shared__ __align__(16) float lds[];
+    double *const worth = reinterpret_cast<double *>(lds);   // [256]
+    float *const zs = lds + 2 * kMaxExperts;                  // [4][Rp], -inf where no expert is
+    float *const zb = zs + kRowsPerWave * P.Rp;               // [Rp], the selection bias
+    short *const pk = reinterpret_cast<short *>(zb + (SCORES ? P.Rp : 0));  // [4][kp]
     const int lane = threadIdx.x, c16 = lane & 15, rr = lane >> 4;
     const int E = P.E, k = P.k, t0 = (int)blockIdx.x * kRowsPerWave;
     const bool sig = (P.flags & PP_SCORE_SIGMOID) != 0;
     const bool top2 = (P.flags & PP_GROUP_TOP2) != 0;
     const bool renorm = (P.flags & PP_TOPK_RENORM) != 0;
+    const bool biased = SCORES && P.sel_bias;
     const int kp = (k + 15) & ~15;
-    auto place = [&](int e) {
-        const int g = (int)((__umul24((uint32_t)e, P.by_Gs)) >> 16);
-        return g * P.Gp + e - g * P.Gs;
-    };
-    // the lane's group, its first value's expert and whether value q exists
-    const int grp = c16 / P.lanes, sub = c16 & (P.lanes - 1);
-    const bool some = grp < P.n_groups;
-    auto has = [&](int q) { return some && q * P.lanes + sub < P.Gs; };
-    auto expert = [&](int q) { return grp * P.Gs + q * P.lanes + sub; };
-    float b[NQ];
-    if (SCORES && P.sel_bias) {
-#pragma unroll
-        for (int q = 0; q < NQ; ++q) b[q] = P.sel_bias[has(q) ? expert(q) : 0];
+    constexpr int NE = kMaxExperts / 64;
+    if (P.pad) {
+        const int n4 = (kRowsPerWave + (SCORES ? 1 : 0)) * P.Rp / 4;
+        for (int i = lane; i < n4; i += 64)
+            reinterpret_cast<float4 *>(zs)[i] =
+                make_float4(-INFINITY, -INFINITY, -INFINITY, -INFINITY);
     }
-    // four rows to LDS, every load issued first
-    {
-        float v[kRowsPerWave][kMaxExperts / 64];
-        if (P.src.g) {
+    // the bias and four rows to LDS, every load issued first
+    if (P.src.g) {
+        float v[kRowsPerWave + 1][NE];
+        if (biased) {
 #pragma unroll
-            for (int r = 0; r < kRowsPerWave; ++r) {
-                const float *row = P.src.g + (size_t)min(t0 + r, P.T - 1) * E;
-#pragma unroll
-                for (int q = 0; q < kMaxExperts / 64; ++q)
-                    if (64 * q < E) v[r][q] = row[min(lane + 64 * q, E - 1)];
-            }
-        } else {
-#pragma unroll
-            for (int r = 0; r < kRowsPerWave; ++r) {
-                const int t = min(t0 + r, P.T - 1);
-                const float it = P.src.inv_temp ? P.src.inv_temp[t] : 1.0f;
-#pragma unroll
-                for (int q = 0; q < kMaxExperts / 64; ++q) {
-                    if (64 * q >= E) continue;
-                    const int e = min(lane + 64 * q, E - 1);
-                    float part[kMaxSlices];
-#pragma unroll
-                    for (int i = 0; i < kMaxSlices; ++i)
-                        part[i] = P.src.gpart[((size_t)min(i, P.src.KSr - 1) * P.T + t) * E + e];
-                    float sum = 0.0f;
-#pragma unroll
-                    for (int i = 0; i < kMaxSlices; ++i)
-                        if (i < P.src.KSr) sum += part[i];
-                    v[r][q] = (sum + P.src.bias[e]) * it;
-                    if (P.src.logits && t0 + r < P.T && lane + 64 * q < E)
-                        P.src.logits[(size_t)t * E + e] = v[r][q];
-                }
-            }
+            for (int q = 0; q < NE; ++q) v[kRowsPerWave][q] = P.sel_bias[min(lane + 64 * q, E - 1)];
         }
 #pragma unroll
-        for (int q = 0; q < kMaxExperts / 64; ++q) {
+        for (int r = 0; r < kRowsPerWave; ++r) {
+            const float *row = P.src.g + (size_t)min(t0 + r, P.T - 1) * E;
+#pragma unroll
+            for (int q = 0; q < NE; ++q) v[r][q] = row[min(lane + 64 * q, E - 1)];
+        }
+#pragma unroll
+        for (int q = 0; q < NE; ++q) {
             const int e = lane + 64 * q;
-            if (e >= E) continue;
-            const int at = place(e);
+            if (e >= E) break;
+            const int at = topk_place(P, e);
 #pragma unroll
             for (int r = 0; r < kRowsPerWave; ++r) zs[r * P.Rp + at] = clean_logit(v[r][q]);
+            if (biased) zb[at] = clean_logit(v[kRowsPerWave][q]);
+        }
+    } else {
+#pragma unroll 1
+        for (int e = lane; e < E; e += 64) {
+            const int at = topk_place(P, e);
+            const float be = P.src.bias[e];
+            if (biased) zb[at] = clean_logit(P.sel_bias[e]);
+#pragma unroll 1
+            for (int r = 0; r < kRowsPerWave; ++r) {
+                const int t = min(t0 + r, P.T - 1);
+                const float *p = P.src.gpart + (size_t)t * E + e;
+                const size_t slice = (size_t)P.T * E;
+                float part[kMaxSlices];
+#pragma unroll
+                for (int i = 0; i < kMaxSlices; ++i) part[i] = p[min(i, P.src.KSr - 1) * slice];
+                float sum = 0.0f;
+#pragma unroll
+                for (int i = 0; i < kMaxSlices; ++i)
+                    if (i < P.src.KSr) sum += part[i];
+                const float z = (sum + be) * (P.src.inv_temp ? P.src.inv_temp[t] : 1.0f);
+                if (P.src.logits && t0 + r < P.T) P.src.logits[(size_t)t * E + e] = z;
+                zs[r * P.Rp + at] = clean_logit(z);
+            }
         }
     }
     __syncthreads();
     const float *const zr = zs + rr * P.Rp;
-    float z[NQ], zmax = -INFINITY;
+    // the lane's group and its first value
+    const int grp = c16 >> P.lanes_log, sub = c16 & (P.lanes - 1);
+    const float *const mz = zr + grp * P.Gp + sub;
+    float c[NQ], zmax = -INFINITY;
 #pragma unroll
     for (int q = 0; q < NQ; ++q) {
-        z[q] = zr[has(q) ? grp * P.Gp + q * P.lanes + sub : 0];
-        z[q] = has(q) ? z[q] : -INFINITY;
-        zmax = fmaxf(zmax, z[q]);
+        c[q] = mz[q * P.lanes];
+        zmax = fmaxf(zmax, c[q]);
     }
     zmax = row_max(zmax);
-    // sum of e^(z - zmax), where softmax scores are wanted
+    // 1 / sum of e^(z - zmax), where softmax weights are wanted as they are
     float Sinv = 0.0f;
-    double Sinv64 = 0.0;
-    C c[NQ];
+    if (!sig && !renorm) {
+        float S = 0.0f;
+#pragma unroll
+        for (int q = 0; q < NQ; ++q) S += exp_fast(c[q] - zmax);
+        Sinv = 1.0f / row_sum(S);  // a row of no experts has no weights
+    }
+    bool unsure = false;  // whether 32 bits do not make the choice
+    float err = 0.0f;     // of c
     if constexpr (SCORES) {
-        double s[NQ], S = 0.0;
+        float big = 0.0f;
+        const float *const mb = zb + grp * P.Gp + sub;
+        if (!biased || sig) {
 #pragma unroll
-        for (int q = 0; q < NQ; ++q) {
-            s[q] = 0.0;
-            if (sig)
-                s[q] = sigmoid64(z[q] > -INFINITY ? z[q] : 0.0f);
-            else if (z[q] > -INFINITY)
-                s[q] = exp_neg((double)z[q] - (double)zmax);
-            if (!sig) S += s[q];
-        }
-        if (!sig) {
-            S = row_sum(S);
-            Sinv64 = S > 0.0 ? rcp64(S) : 0.0;
-            Sinv = (float)Sinv64;
-        }
-#pragma unroll
-        for (int q = 0; q < NQ; ++q) {
-            if (!sig) s[q] *= Sinv64;
-            if (P.sel_bias) {
-                b[q] = clean_logit(b[q]);
-                s[q] += (double)b[q];
-                c[q] = z[q] > -INFINITY && b[q] > -INFINITY ? s[q] : -INFINITY;
-            } else {
-                c[q] = z[q] > -INFINITY ? s[q] : -INFINITY;
+            for (int q = 0; q < NQ; ++q) {
+                float v = sig ? sigmoid_fast(c[q]) : exp_fast(c[q] - zmax);
+                float b = 0.0f;
+                if (biased) {
+                    b = mb[q * P.lanes];
+                    v += b;
+                }
+                // computed for every lane, not in a branch of its own
+                asm volatile("" : "+v"(v));
+                c[q] = fminf(c[q], b) > -INFINITY ? v : -INFINITY;
+                big = fmaxf(big, c[q] > -INFINITY ? fabsf(v) : 0.0f);
             }
-        }
-    } else {
-#pragma unroll
-        for (int q = 0; q < NQ; ++q) c[q] = z[q];
-        if (!sig && !renorm) {
-            float S = 0.0f;
-#pragma unroll
-            for (int q = 0; q < NQ; ++q) S += z[q] > -INFINITY ? exp_fast(z[q] - zmax) : 0.0f;
-            S = row_sum(S);
-            Sinv = S > 0.0f ? 1.0f / S : 0.0f;
+            // the score's error and the rounding of the sum with the bias
+            err = kScoreErr + row_max(big) * 2.4e-7f;
+        } else {
+            unsure = true;  // softmax plus a bias needs every score in 64 bits
         }
     }
-    // groups: values of those that go become -inf
+    // the groups that stay
     if (P.n_groups > 1) {
-        C a = -INFINITY, n = -INFINITY;  // the two largest
+        float a = -INFINITY, n = -INFINITY;  // the two largest
 #pragma unroll
         for (int q = 0; q < NQ; ++q) {
-            n = max(n, min(a, c[q]));
-            a = max(a, c[q]);
+            n = __builtin_amdgcn_fmed3f(n, a, c[q]);  // n <= a: the middle one
+            a = fmaxf(a, c[q]);
         }
-        auto join = [&](C a2, C n2) {
-            n = max(min(a, a2), max(n, n2));
-            a = max(a, a2);
+        auto join = [&](float a2, float n2) {
+            n = fmaxf(fminf(a, a2), fmaxf(n, n2));
+            a = fmaxf(a, a2);
         };
         if (P.lanes > 1) join(row_lane<kX1>(a), row_lane<kX1>(n));
         if (P.lanes > 2) join(row_lane<kX2>(a), row_lane<kX2>(n));
         if (P.lanes > 4) join(row_lane<kX4>(a), row_lane<kX4>(n));
-        const C v = top2 && n > -INFINITY ? a + n : a;
-        int front = 0;  // lanes of better groups
+        const float v = top2 && n > -INFINITY ? a + n : a;
+        // groups in front, and those that might be if each worth is off by
+        // what its two scores and their sum are
+        const float off = SCORES ? 3.0f * err : 0.0f;
+        int front = 0, near = 0;
         each_rotation([&](auto ctrl) {
-            const C o = row_lane<decltype(ctrl)::value>(v);
-            const int og = (int)row_u32<decltype(ctrl)::value>((uint32_t)grp);
-            front += (o > v || (o == v && og < grp)) ? 1 : 0;
+            constexpr int R = decltype(ctrl)::value;
+            if ((R & (P.lanes - 1)) != 0) return;  // from group to group
+            const float o = row_lane<R>(v);
+            if constexpr (SCORES) {
+                front += o > v + off ? 1 : 0;
+                near += o >= v - off ? 1 : 0;
+            } else {
+                // rotated by R: lane c reads lane c + 16 - R (or c - R)
+                const bool before = (int)row_u32<R>((uint32_t)grp) < grp;
+                front += o > v || (o == v && before) ? 1 : 0;
+            }
         });
-        if (front >= P.top_groups * P.lanes) {
+        if (SCORES)
+            unsure |= v > -INFINITY && front < P.top_groups && near >= P.top_groups;
+        const bool out = front >= P.top_groups;
 #pragma unroll
-            for (int q = 0; q < NQ; ++q) c[q] = -INFINITY;
+        for (int q = 0; q < NQ; ++q) c[q] = out ? -INFINITY : c[q];
+    }
+    if (SCORES && !biased) {  // then experts are in the order of the logits
+        err = 0.0f;
+#pragma unroll
+        for (int q = 0; q < NQ; ++q) {
+            const float z = mz[q * P.lanes];
+            c[q] = c[q] > -INFINITY ? z : -INFINITY;
         }
     }
-    if constexpr (SCORES) {
-        // without a bias the experts are in the order of the logits: scores
-        // that round to the same number are not equal
-        if (!P.sel_bias) {
-#pragma unroll
-            for (int q = 0; q < NQ; ++q) c[q] = c[q] > -INFINITY ? (double)z[q] : -INFINITY;
-        }
-    }
-    C cmax = -INFINITY;
-#pragma unroll
-    for (int q = 0; q < NQ; ++q) cmax = max(cmax, c[q]);
-    cmax = row_max(cmax);
     constexpr uint32_t kNone = 0xFFFFFFFFu;
     uint32_t key[NQ];
+    {
+        float cmax = c[0];
 #pragma unroll
-    for (int q = 0; q < NQ; ++q) {
-        const uint32_t d = __float_as_uint((float)(cmax - c[q]));
-        key[q] = c[q] > -INFINITY ? ((d & 0xFFFFFF00u) | (uint32_t)expert(q)) : kNone;
+        for (int q = 1; q < NQ; ++q) cmax = fmaxf(cmax, c[q]);
+        cmax = row_max(cmax);
+        uint32_t e = (uint32_t)(grp * P.Gs + sub);
+#pragma unroll
+        for (int q = 0; q < NQ; ++q) {
+            const uint32_t d = __float_as_uint(cmax - c[q]) & 0xFFFFFF00u;
+            key[q] = c[q] > -INFINITY ? d | e : kNone;
+            e += (uint32_t)P.lanes;
+        }
     }
     // the next key after `last`: the smallest of key - last - 1, where keys
     // up to `last` wrap to the top
     auto next_key = [&](uint32_t last) {
-        uint32_t m = kNone;
+        uint32_t m = key[0] + ~last;
 #pragma unroll
-        for (int q = 0; q < NQ; ++q) m = min(m, key[q] - last - 1u);
+        for (int q = 1; q < NQ; ++q) m = min(m, key[q] + ~last);
         return row_min(m) + last + 1u;
     };
     uint32_t mine = kNone, last = kNone;
-    bool close = false;  // two neighbours of the list with equal upper bits
+    bool close = biased;  // whether the list's order may not be that of c
+#pragma unroll 1
     for (int j = 0; j < k; ++j) {
         // a list that has ended stays at kNone: the subtraction would wrap
         const bool over = j > 0 && last == kNone;
         const uint32_t n = next_key(last);
-        close |= !over && n != kNone && j > 0 && ((n ^ last) < 256u);
+        close |= !over && n != kNone && j > 0 && (n ^ last) < 256u;
         last = over ? kNone : n;
         mine = c16 == (j & 15) ? last : mine;
         if ((j & 15) == 15 || j == k - 1) {
@@ -358,69 +497,51 @@ __global__ __launch_bounds__(64) void route_topk_k(TopkParams P) {
             if (j != k - 1) mine = kNone;
         }
     }
-    // entries past the cut that share the upper bits of the last one
-    bool full = false;
+    // entries past the cut that may belong in front of it: their distance from
+    // the largest c is not certainly more than that of the last one (2^-15 of
+    // it was cut off, and twice err)
     {
-        const uint32_t bucket = last;
+        const float cut = __uint_as_float(last & 0xFFFFFF00u) * 1.0001f + 2.0f * err;
         int m = k;
         bool more = last != kNone;
         while (true) {
             const uint32_t n = next_key(last);
-            more = more && n > last && n != kNone && ((n ^ bucket) < 256u);
+            more = more && n > last && n != kNone && __uint_as_float(n & 0xFFFFFF00u) <= cut;
             if (__ballot(more) == 0ull) break;
             close |= more;
             if (m >= 16) {
-                full |= more;
+                unsure |= more;
                 break;
             }
             last = more ? n : last;
             if (more && c16 == m) mine = n;
             ++m;
         }
-        full |= close && k > 16;
+        unsure |= close && k > 16;
     }
     if (__ballot(close) != 0ull) {
-        if (__ballot(full) == 0ull) {
-            // up to 16 candidates, one a lane, by their c
-            const bool cand = mine != kNone;
-            const int e = cand ? (int)(mine & 255u) : 0;
-            double v = -INFINITY;
-            if (cand) {
-                const float x = zr[place(e)];
-                v = (double)x;
-                if (SCORES && P.sel_bias) {
-                    const double s = sig ? sigmoid64(x)
-                                         : exp_neg((double)x - (double)zmax) * Sinv64;
-                    v = s + (double)clean_logit(P.sel_bias[e]);
-                }
-            }
-            int rank = 0;
-            const uint32_t order = cand ? (uint32_t)e : 256u + (uint32_t)c16;
-            each_rotation([&](auto ctrl) {
-                const double o = row_lane<decltype(ctrl)::value>(v);
-                const uint32_t oe = row_u32<decltype(ctrl)::value>(order);
-                rank += (o > v || (o == v && oe < order)) ? 1 : 0;
-            });
-            if (rank < k) pk[rr * kp + rank] = cand ? (short)e : (short)-1;
-        } else {
-            // the row's choice from all its c
-            for (int j = 0; j < k; ++j) {
-                C best = -INFINITY;
-                int be = 256;
-#pragma unroll
-                for (int q = 0; q < NQ; ++q) {
-                    const bool up = c[q] > best;
-                    best = up ? c[q] : best;
-                    be = up ? expert(q) : be;
-                }
-                const C top = row_max(best);
-                const int e = (int)row_min(best == top && top > -INFINITY ? (uint32_t)be : 256u);
-                if (c16 == 0) pk[rr * kp + j] = e < 256 ? (short)e : (short)-1;
-#pragma unroll
-                for (int q = 0; q < NQ; ++q)
-                    if (expert(q) == e && has(q)) c[q] = -INFINITY;
-            }
-        }
+        // up to 16 candidates, one a lane, by their c (not used for k > 16)
+        const bool cand = mine != kNone && k <= 16;
+        const int e = cand ? (int)(mine & 255u) : 0;
+        const float x = zr[topk_place(P, e)];
+        double v = (double)x;
+        if (biased) v = sigmoid64(x) + (double)zb[topk_place(P, e)];
+        v = cand ? v : -INFINITY;
+        int rank = 0;
+        const uint32_t order = cand ? (uint32_t)e : 256u + (uint32_t)c16;
+        each_rotation([&](auto ctrl) {
+            const double o = row_lane<decltype(ctrl)::value>(v);
+            const uint32_t oe = row_u32<decltype(ctrl)::value>(order);
+            rank += o > v || (o == v && oe < order) ? 1 : 0;
+        });
+        if (rank < k && k <= 16) pk[rr * kp + rank] = cand ? (short)e : (short)-1;
+    }
+    const unsigned long long open = __ballot(unsure);
+    if (open != 0ull) {
+#pragma unroll 1
+        for (int r = 0; r < kRowsPerWave; ++r)
+            if ((open >> (16 * r)) & 0xFFFFull)
+                choose_row(P, zs + r * P.Rp, zb, __shfl(zmax, 16 * r, 64), worth, pk + r * kp, lane);
     }
     __syncthreads();
     // weights
@@ -429,14 +550,14 @@ __global__ __launch_bounds__(64) void route_topk_k(TopkParams P) {
         m = -INFINITY;
         for (int j = c16; j < k; j += 16) {
             const int e = pk[rr * kp + j];
-            if (e >= 0) m = fmaxf(m, zr[place(e)]);
+            if (e >= 0) m = fmaxf(m, zr[topk_place(P, e)]);
         }
         m = row_max(m);
         if (sig) m = fminf(m, 0.0f);
         float tot = 0.0f;
         for (int j = c16; j < k; j += 16) {
             const int e = pk[rr * kp + j];
-            if (e >= 0) tot += sig ? rel_sigmoid(zr[place(e)], m) : expf(zr[place(e)] - m);
+            if (e >= 0) tot += sig ? rel_sigmoid(zr[topk_place(P, e)], m) : expf(zr[topk_place(P, e)] - m);
         }
         tot = row_sum(tot);
         scale = P.scale / tot;  // rows of empty slots do not use it
@@ -447,7 +568,7 @@ __global__ __launch_bounds__(64) void route_topk_k(TopkParams P) {
         const int e = pk[rr * kp + j];
         float w = 0.0f;
         if (e >= 0) {
-            const float x = zr[place(e)];
+            const float x = zr[topk_place(P, e)];
             w = scale * (sig ? rel_sigmoid(x, m) : expf(x - m));
         }
         P.idx[(size_t)t * k + j] = e;
@@ -573,42 +694,40 @@ pp_status check_rule(int32_t E, int32_t k, int32_t n_groups, int32_t top_groups,
     return PP_OK;
 }
 
-// Values a lane holds of E experts in n_groups groups: 16 for 256 experts in
-// one group, at most 28 (nine groups of 28 on a lane each).
-constexpr int kLaneValues[] = {1, 2, 3, 4, 5, 6, 7, 8, 10, 12, 14, 16, 20, 28};
-
+// The builds by how many values a lane holds: 16 for 256 experts in one group.
+struct TopkBuild {
+    int values;
+    void (*scores)(TopkParams);
+    void (*logits)(TopkParams);
+};
 template <int NQ>
-void launch_topk_nq(const TopkParams &P, bool scores, size_t lds, hipStream_t s) {
-    const dim3 grid((P.T + kRowsPerWave - 1) / kRowsPerWave);
-    if (scores)
-        hipLaunchKernelGGL((route_topk_k<NQ, true>), grid, dim3(64), lds, s, P);
-    else
-        hipLaunchKernelGGL((route_topk_k<NQ, false>), grid, dim3(64), lds, s, P);
+constexpr TopkBuild topk_build() {
+    return {NQ, route_topk_k<NQ, true>, route_topk_k<NQ, false>};
 }
-template <int... I>
-bool launch_topk_for(int need, const TopkParams &P, bool scores, size_t lds, hipStream_t s,
-                     std::integer_sequence<int, I...>) {
-    return (... || (need <= kLaneValues[I]
-                        ? (launch_topk_nq<kLaneValues[I]>(P, scores, lds, s), true)
-                        : false));
-}
+constexpr TopkBuild kTopkBuilds[] = {
+    topk_build<1>(),  topk_build<2>(),  topk_build<3>(),  topk_build<4>(),  topk_build<5>(),
+    topk_build<6>(),  topk_build<7>(),  topk_build<8>(),  topk_build<10>(), topk_build<12>(),
+    topk_build<14>(), topk_build<16>(), topk_build<20>(), topk_build<28>()};
 
 hipError_t launch_topk(TopkParams P, hipStream_t s) {
-    int p2 = 1;
-    while (p2 < P.n_groups) p2 *= 2;
     P.Gs = P.E / P.n_groups;
-    P.lanes = 16 / p2;
+    P.lanes_log = 4;
+    while ((16 >> P.lanes_log) < P.n_groups) --P.lanes_log;
+    P.lanes = 1 << P.lanes_log;
+    const TopkBuild *B = kTopkBuilds;
+    while (B->values * P.lanes < P.Gs) ++B;  // at most 28: nine groups of 28, a lane each
     // a group starts `lanes` banks after the one before, so that the 16 lanes
     // of a row read 16 different banks; one group: rows 16 banks apart
-    P.Gp = (P.Gs + 31) / 32 * 32 + P.lanes;
-    P.Rp = p2 * P.Gp;
+    P.Gp = (B->values * P.lanes + 31) / 32 * 32 + P.lanes;
+    P.Rp = (16 >> P.lanes_log) * P.Gp;
     P.by_Gs = (uint32_t)((65536 + P.Gs - 1) / P.Gs);
+    P.pad = P.n_groups << P.lanes_log != 16 || B->values * P.lanes != P.Gs;
     const bool scores = P.sel_bias || (P.n_groups > 1 && (P.flags & PP_GROUP_TOP2));
-    const size_t lds = sizeof(float) * 4 * P.Rp + sizeof(short) * 4 * ((P.k + 15) & ~15);
-    constexpr int n = sizeof(kLaneValues) / sizeof(kLaneValues[0]);
-    if (!launch_topk_for((P.Gs + P.lanes - 1) / P.lanes, P, scores, lds, s,
-                         std::make_integer_sequence<int, n>{}))
-        return hipErrorInvalidValue;
+    const size_t lds = sizeof(double) * kMaxExperts +
+                       sizeof(float) * (kRowsPerWave + (scores ? 1 : 0)) * P.Rp +
+                       sizeof(short) * kRowsPerWave * ((P.k + 15) & ~15);
+    hipLaunchKernelGGL(scores ? B->scores : B->logits,
+                       dim3((P.T + kRowsPerWave - 1) / kRowsPerWave), dim3(64), lds, s, P);
     return hipGetLastError();
 }
 
@@ -634,7 +753,7 @@ extern "C" pp_status prunepath_route_topk(pp_layer *L, const uint16_t *x, int32_
     if (e == hipSuccess) {
         const RouteParams R = route_params(L, x, T, 0.0f, inv_temp, nullptr, nullptr, nullptr, false);
         const TopkParams P = {{nullptr, R.gpart, R.bias, inv_temp, logits, R.KSr}, T, E, k, n_groups,
-                              top_groups, sel_bias, scale, flags, expert_idx, gate_w, 0, 0, 0, 0, 0};
+                              top_groups, sel_bias, scale, flags, expert_idx, gate_w, 0, 0, 0, 0, 0, 0, 0};
         prof_mark(L, PP_KERNEL_ROUTE, s, true);
         e = launch_topk(P, s);
         prof_mark(L, PP_KERNEL_ROUTE, s, false);
@@ -653,7 +772,7 @@ extern "C" pp_status prunepath_route_topk_logits(const float *g, int32_t T, int3
         check_rule(E, k, n_groups, top_groups, sel_bias, scale, flags, expert_idx, gate_w);
     if (st != PP_OK) return st;
     const TopkParams P = {{g, nullptr, nullptr, nullptr, nullptr, 0}, T, E, k, n_groups, top_groups,
-                          sel_bias, scale, flags, expert_idx, gate_w, 0, 0, 0, 0, 0};
+                          sel_bias, scale, flags, expert_idx, gate_w, 0, 0, 0, 0, 0, 0, 0};
     return launch_topk(P, static_cast<hipStream_t>(hip_stream)) == hipSuccess ? PP_OK : PP_EHIP;
 }
 
