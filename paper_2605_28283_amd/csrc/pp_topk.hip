@@ -9,8 +9,7 @@
 //   Chosen: the k largest c of the groups that stay, equal ones by ascending
 //   index.  w_j = scale s_j, or scale s_j / (sum of the chosen s).
 //
-// A token takes the 16 lanes of one DPP row, four tokens a wavefront, one
-// wavefront a workgroup.  The rows of logits (and the bias) are read in whole
+// A token takes the 16 lanes of one DPP row, four tokens a wavefront.  The rows of logits (and the bias) are read in whole
 // cache lines into LDS; a lane then holds values of one group only (16 lanes
 // over the next power of two of n_groups), so a group's worth is a reduction
 // in registers and over few lanes.
@@ -35,7 +34,9 @@ namespace pp {
 namespace {
 
 constexpr int kRowsPerWave = 4;
+constexpr int kTopkWaves = 4;    // of a workgroup (single ones are not dispatched fast enough)
 constexpr int kMaxGroups = 16;
+constexpr int kMaxList = 64;     // entries put in order in 64 bits
 constexpr int kMaxTopkRows = 1 << 22;
 constexpr float kFltMax = 3.402823466e38f;
 
@@ -65,6 +66,8 @@ struct TopkParams {
     int Gp, Rp;      // LDS floats from group to group, from row to row
     uint32_t by_Gs;  // ceil(2^16 / Gs): e / Gs = (e by_Gs) >> 16 for e < 256
     int pad;         // whether lanes read places without an expert
+    int kp;          // list entries of a row in LDS: k, and room to kMaxList
+    int wave_lds;    // floats of a wavefront
 };
 
 // NaN and -inf to -inf, +inf to the largest float.
@@ -207,10 +210,52 @@ __device__ __forceinline__ uint32_t wave_min_u32(uint32_t v, int lane) {
     return min(v, xor_lane<32>(v, lane));
 }
 
+// A wavefront's LDS is its own: its operations on it are carried out in order,
+// and this keeps the compiler from changing that order.
+__device__ __forceinline__ void wave_sync() {
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+}
+
+// Logit of token t and expert e, from the router's partial sums (and stored
+// for the caller, if it wants them).
+__device__ __forceinline__ float summed_logit(const TopkParams &P, int t, int e, bool store) {
+    const float *p = P.src.gpart + (size_t)t * P.E + e;
+    const size_t slice = (size_t)P.T * P.E;
+    float part[kMaxSlices];
+#pragma unroll
+    for (int i = 0; i < kMaxSlices; ++i) part[i] = p[min(i, P.src.KSr - 1) * slice];
+    float sum = 0.0f;
+#pragma unroll
+    for (int i = 0; i < kMaxSlices; ++i)
+        if (i < P.src.KSr) sum += part[i];
+    const float z = (sum + P.src.bias[e]) * (P.src.inv_temp ? P.src.inv_temp[t] : 1.0f);
+    if (P.src.logits && store) P.src.logits[(size_t)t * P.E + e] = z;
+    return z;
+}
+
 // e's place in a row in LDS.
 __device__ __forceinline__ int topk_place(const TopkParams &P, int e) {
     const int g = (int)(__umul24((uint32_t)e, P.by_Gs) >> 16);
     return g * P.Gp + e - g * P.Gs;
+}
+
+// Puts the n <= 64 listed experts in order of c (equal ones by index), of
+// which the first k are kept.
+__device__ __forceinline__ void sort_list(const double *c, short *list, int n, int k, int lane) {
+    wave_sync();
+    const int e = list[min(lane, n - 1)];
+    const double v = c[e];
+    int rank = 0;
+#pragma unroll 4
+    for (int j = 0; j < n; ++j) {
+        const int oe = list[j];
+        const double o = c[oe];
+        rank += o > v || (o == v && oe < e) ? 1 : 0;
+    }
+    wave_sync();
+    if (lane < n && rank < k) list[rank] = (short)e;
+    wave_sync();
 }
 
 // One row's choice, all of it in 64 bits, by the whole wavefront: lane l has
@@ -250,7 +295,7 @@ __device__ __forceinline__ void choose_row(const TopkParams &P, const float *zr,
             worth[e] = top2 && !P.sel_bias && c[q] > -INFINITY ? s[q] : c[q];
     }
     if (P.n_groups > 1) {
-        __syncthreads();
+        wave_sync();
         double a = -INFINITY, n = -INFINITY;
         if (lane < P.n_groups) {
 #pragma unroll 4
@@ -261,9 +306,9 @@ __device__ __forceinline__ void choose_row(const TopkParams &P, const float *zr,
             }
             if (top2 && n > -INFINITY) a += n;
         }
-        __syncthreads();
+        wave_sync();
         worth[lane] = a;
-        __syncthreads();
+        wave_sync();
         int front = 0;
 #pragma unroll 1
         for (int g = 0; g < P.n_groups; ++g) {
@@ -271,7 +316,7 @@ __device__ __forceinline__ void choose_row(const TopkParams &P, const float *zr,
             front += o > a || (o == a && g < lane) ? 1 : 0;
         }
         const unsigned long long stay = __ballot(front < P.top_groups && lane < P.n_groups);
-        __syncthreads();  // worth is free again
+        wave_sync();  // worth is free again
 #pragma unroll
         for (int q = 0; q < NE; ++q) {
             const int g = (int)(__umul24((uint32_t)(lane + 64 * q), P.by_Gs) >> 16);
@@ -298,22 +343,69 @@ __device__ __forceinline__ void choose_row(const TopkParams &P, const float *zr,
     }
 }
 
+// Weights of a row's choice, by W lanes, and the choice itself.  zr: the row
+// in LDS; zmax: its largest logit; Sinv: 1 / (sum of e^(z - zmax)).
+template <int W>
+__device__ __forceinline__ void store_row(const TopkParams &P, const float *zr, float zmax,
+                                          float Sinv, const short *list, int t, int l) {
+    const bool sig = (P.flags & PP_SCORE_SIGMOID) != 0;
+    const int k = P.k;
+    float m = sig ? 0.0f : zmax, scale = sig ? P.scale : P.scale * Sinv;
+    if (P.flags & PP_TOPK_RENORM) {
+        // sums over each 16 lanes, then over the rows of 16
+        m = -INFINITY;
+        for (int j = l; j < k; j += W) {
+            const int e = list[j];
+            if (e >= 0) m = fmaxf(m, zr[topk_place(P, e)]);
+        }
+        m = row_max(m);
+        if (W == 64) {
+            m = fmaxf(m, __uint_as_float(xor_lane<16>(__float_as_uint(m), l)));
+            m = fmaxf(m, __uint_as_float(xor_lane<32>(__float_as_uint(m), l)));
+        }
+        if (sig) m = fminf(m, 0.0f);
+        float tot = 0.0f;
+        for (int j = l & 15; j < k; j += 16) {
+            const int e = list[j];
+            if (e >= 0) {
+                const float x = zr[topk_place(P, e)];
+                tot += sig ? rel_sigmoid(x, m) : expf(x - m);
+            }
+        }
+        // every 16 lanes take all slots, in the same order for either W
+        scale = P.scale / row_sum(tot);  // rows of empty slots do not use it
+    }
+    for (int j = l; j < k; j += W) {
+        const int e = list[j];
+        float w = 0.0f;
+        if (e >= 0) {
+            const float x = zr[topk_place(P, e)];
+            w = scale * (sig ? rel_sigmoid(x, m) : expf(x - m));
+        }
+        P.idx[(size_t)t * k + j] = e;
+        P.w[(size_t)t * k + j] = w;
+    }
+}
+
 // NQ: values a lane holds.  SCORES: scores decide (a bias, or groups worth two
 // scores); else c is the logit and needs no 64 bits.
 template <int NQ, bool SCORES>
-__global__ __launch_bounds__(64) void route_topk_k(TopkParams P) {
-    extern __shared__ __align__(16) float lds[];
+__global__ __launch_bounds__(64 * kTopkWaves) void route_topk_k(TopkParams P) {
+    extern __shared__ __align__(16) float all_lds[];
+    float *const lds = all_lds + (threadIdx.x >> 6) * P.wave_lds;
     double *const worth = reinterpret_cast<double *>(lds);   // [256]
     float *const zs = lds + 2 * kMaxExperts;                  // [4][Rp], -inf where no expert is
     float *const zb = zs + kRowsPerWave * P.Rp;               // [Rp], the selection bias
     short *const pk = reinterpret_cast<short *>(zb + (SCORES ? P.Rp : 0));  // [4][kp]
-    const int lane = threadIdx.x, c16 = lane & 15, rr = lane >> 4;
-    const int E = P.E, k = P.k, t0 = (int)blockIdx.x * kRowsPerWave;
+    const int lane = threadIdx.x & 63, c16 = lane & 15, rr = lane >> 4;
+    const int E = P.E, k = P.k;
+    const int t0 = (int)(blockIdx.x * kTopkWaves + (threadIdx.x >> 6)) * kRowsPerWave;
+    if (t0 >= P.T) return;
     const bool sig = (P.flags & PP_SCORE_SIGMOID) != 0;
     const bool top2 = (P.flags & PP_GROUP_TOP2) != 0;
     const bool renorm = (P.flags & PP_TOPK_RENORM) != 0;
     const bool biased = SCORES && P.sel_bias;
-    const int kp = (k + 15) & ~15;
+    const int kp = P.kp;
     constexpr int NE = kMaxExperts / 64;
     if (P.pad) {
         const int n4 = (kRowsPerWave + (SCORES ? 1 : 0)) * P.Rp / 4;
@@ -347,27 +439,14 @@ __global__ __launch_bounds__(64) void route_topk_k(TopkParams P) {
 #pragma unroll 1
         for (int e = lane; e < E; e += 64) {
             const int at = topk_place(P, e);
-            const float be = P.src.bias[e];
             if (biased) zb[at] = clean_logit(P.sel_bias[e]);
 #pragma unroll 1
-            for (int r = 0; r < kRowsPerWave; ++r) {
-                const int t = min(t0 + r, P.T - 1);
-                const float *p = P.src.gpart + (size_t)t * E + e;
-                const size_t slice = (size_t)P.T * E;
-                float part[kMaxSlices];
-#pragma unroll
-                for (int i = 0; i < kMaxSlices; ++i) part[i] = p[min(i, P.src.KSr - 1) * slice];
-                float sum = 0.0f;
-#pragma unroll
-                for (int i = 0; i < kMaxSlices; ++i)
-                    if (i < P.src.KSr) sum += part[i];
-                const float z = (sum + be) * (P.src.inv_temp ? P.src.inv_temp[t] : 1.0f);
-                if (P.src.logits && t0 + r < P.T) P.src.logits[(size_t)t * E + e] = z;
-                zs[r * P.Rp + at] = clean_logit(z);
-            }
+            for (int r = 0; r < kRowsPerWave; ++r)
+                zs[r * P.Rp + at] =
+                    clean_logit(summed_logit(P, min(t0 + r, P.T - 1), e, t0 + r < P.T));
         }
     }
-    __syncthreads();
+    wave_sync();
     const float *const zr = zs + rr * P.Rp;
     // the lane's group and its first value
     const int grp = c16 >> P.lanes_log, sub = c16 & (P.lanes - 1);
@@ -392,7 +471,7 @@ __global__ __launch_bounds__(64) void route_topk_k(TopkParams P) {
     if constexpr (SCORES) {
         float big = 0.0f;
         const float *const mb = zb + grp * P.Gp + sub;
-        if (!biased || sig) {
+        {
 #pragma unroll
             for (int q = 0; q < NQ; ++q) {
                 float v = sig ? sigmoid_fast(c[q]) : exp_fast(c[q] - zmax);
@@ -408,8 +487,6 @@ __global__ __launch_bounds__(64) void route_topk_k(TopkParams P) {
             }
             // the score's error and the rounding of the sum with the bias
             err = kScoreErr + row_max(big) * 2.4e-7f;
-        } else {
-            unsure = true;  // softmax plus a bias needs every score in 64 bits
         }
     }
     // the groups that stay
@@ -482,59 +559,59 @@ __global__ __launch_bounds__(64) void route_topk_k(TopkParams P) {
         for (int q = 1; q < NQ; ++q) m = min(m, key[q] + ~last);
         return row_min(m) + last + 1u;
     };
-    uint32_t mine = kNone, last = kNone;
-    bool close = biased;  // whether the list's order may not be that of c
+    // A key's distance from the largest c, and up to which one an entry may
+    // belong in front of it: 2^-15 of each was cut off, and c is off by err.
+    auto distance = [](uint32_t v) { return __uint_as_float(v & 0xFFFFFF00u); };
+    auto reach = [&](uint32_t v) { return distance(v) * 1.0001f + 2.0f * err; };
+    uint32_t last = kNone;
+    bool close = false;  // whether the list's order may not be that of c
+    int len = 0;         // of the row's list
 #pragma unroll 1
     for (int j = 0; j < k; ++j) {
         // a list that has ended stays at kNone: the subtraction would wrap
         const bool over = j > 0 && last == kNone;
         const uint32_t n = next_key(last);
-        close |= !over && n != kNone && j > 0 && (n ^ last) < 256u;
+        close |= !over && n != kNone && j > 0 && distance(n) <= reach(last);
         last = over ? kNone : n;
-        mine = c16 == (j & 15) ? last : mine;
-        if ((j & 15) == 15 || j == k - 1) {
-            pk[rr * kp + (j & ~15) + c16] = mine == kNone ? (short)-1 : (short)(mine & 255u);
-            if (j != k - 1) mine = kNone;
-        }
+        len += last != kNone ? 1 : 0;
+        if (c16 == 0) pk[rr * kp + j] = last != kNone ? (short)(last & 255u) : (short)-1;
     }
-    // entries past the cut that may belong in front of it: their distance from
-    // the largest c is not certainly more than that of the last one (2^-15 of
-    // it was cut off, and twice err)
+    // entries past the cut that may belong in front of it
     {
-        const float cut = __uint_as_float(last & 0xFFFFFF00u) * 1.0001f + 2.0f * err;
-        int m = k;
+        const float cut = reach(last);
         bool more = last != kNone;
-        while (true) {
+        for (int m = k;; ++m) {
             const uint32_t n = next_key(last);
-            more = more && n > last && n != kNone && __uint_as_float(n & 0xFFFFFF00u) <= cut;
+            more = more && n > last && n != kNone && distance(n) <= cut;
             if (__ballot(more) == 0ull) break;
             close |= more;
-            if (m >= 16) {
+            if (m >= kMaxList) {
                 unsure |= more;
                 break;
             }
             last = more ? n : last;
-            if (more && c16 == m) mine = n;
-            ++m;
+            if (more) {
+                if (c16 == 0) pk[rr * kp + m] = (short)(n & 255u);
+                ++len;
+            }
         }
-        unsure |= close && k > 16;
+        unsure |= close && k > kMaxList;
     }
-    if (__ballot(close) != 0ull) {
-        // up to 16 candidates, one a lane, by their c (not used for k > 16)
-        const bool cand = mine != kNone && k <= 16;
-        const int e = cand ? (int)(mine & 255u) : 0;
-        const float x = zr[topk_place(P, e)];
-        double v = (double)x;
-        if (biased) v = sigmoid64(x) + (double)zb[topk_place(P, e)];
-        v = cand ? v : -INFINITY;
-        int rank = 0;
-        const uint32_t order = cand ? (uint32_t)e : 256u + (uint32_t)c16;
-        each_rotation([&](auto ctrl) {
-            const double o = row_lane<decltype(ctrl)::value>(v);
-            const uint32_t oe = row_u32<decltype(ctrl)::value>(order);
-            rank += o > v || (o == v && oe < order) ? 1 : 0;
-        });
-        if (rank < k && k <= 16) pk[rr * kp + rank] = cand ? (short)e : (short)-1;
+    wave_sync();
+    // rows whose list is put in order by c in 64 bits
+    const unsigned long long sort = __ballot(close && !unsure);
+    if (sort != 0ull) {
+#pragma unroll 1
+        for (int r = 0; r < kRowsPerWave; ++r) {
+            if (!((sort >> (16 * r)) & 1ull)) continue;
+            const int n = __builtin_amdgcn_readlane(len, 16 * r);
+            if (lane < n) {
+                const int e = pk[r * kp + lane], at = topk_place(P, e);
+                const float x = zs[r * P.Rp + at];
+                worth[e] = biased ? sigmoid64(x) + (double)zb[at] : (double)x;
+            }
+            sort_list(worth, pk + r * kp, n, k, lane);
+        }
     }
     const unsigned long long open = __ballot(unsure);
     if (open != 0ull) {
@@ -543,37 +620,215 @@ __global__ __launch_bounds__(64) void route_topk_k(TopkParams P) {
             if ((open >> (16 * r)) & 0xFFFFull)
                 choose_row(P, zs + r * P.Rp, zb, __shfl(zmax, 16 * r, 64), worth, pk + r * kp, lane);
     }
-    __syncthreads();
-    // weights
-    float m = sig ? 0.0f : zmax, scale = sig ? P.scale : P.scale * Sinv;
-    if (renorm) {
-        m = -INFINITY;
-        for (int j = c16; j < k; j += 16) {
-            const int e = pk[rr * kp + j];
-            if (e >= 0) m = fmaxf(m, zr[topk_place(P, e)]);
-        }
-        m = row_max(m);
-        if (sig) m = fminf(m, 0.0f);
-        float tot = 0.0f;
-        for (int j = c16; j < k; j += 16) {
-            const int e = pk[rr * kp + j];
-            if (e >= 0) tot += sig ? rel_sigmoid(zr[topk_place(P, e)], m) : expf(zr[topk_place(P, e)] - m);
-        }
-        tot = row_sum(tot);
-        scale = P.scale / tot;  // rows of empty slots do not use it
-    }
+    wave_sync();
     const int t = t0 + rr;
+    if (t < P.T) store_row<16>(P, zr, zmax, Sinv, pk + rr * kp, t, c16);
+}
+
+// One token a wavefront: the same choice, made in 64 bits at once, for few
+// tokens (a wavefront's work is spread over 64 lanes: 64 tokens of 256 experts
+// in 8 groups MEASURE_WIDE us) and for softmax scores plus a bias, which need
+// every score in 64 bits.  A group has 64 lanes over the next power of two of
+// n_groups; the passes' minimum is a scalar.
+template <int NQ>
+__global__ __launch_bounds__(64 * kTopkWaves) void route_topk_wide_k(TopkParams P) {
+    extern __shared__ __align__(16) float all_lds[];
+    float *const lds = all_lds + (threadIdx.x >> 6) * P.wave_lds;
+    double *const cs = reinterpret_cast<double *>(lds);       // [256]
+    float *const zs = lds + 2 * kMaxExperts;                  // [256]
+    float *const zb = zs + kMaxExperts;                       // [256]
+    short *const pk = reinterpret_cast<short *>(zb + kMaxExperts);  // [kp]
+    const int lane = threadIdx.x & 63;
+    const int t = (int)(blockIdx.x * kTopkWaves + (threadIdx.x >> 6));
     if (t >= P.T) return;
-    for (int j = c16; j < k; j += 16) {
-        const int e = pk[rr * kp + j];
-        float w = 0.0f;
-        if (e >= 0) {
-            const float x = zr[topk_place(P, e)];
-            w = scale * (sig ? rel_sigmoid(x, m) : expf(x - m));
+    const int E = P.E, k = P.k;
+    const bool sig = (P.flags & PP_SCORE_SIGMOID) != 0;
+    const bool top2 = (P.flags & PP_GROUP_TOP2) != 0;
+    const bool biased = P.sel_bias != nullptr;
+    const bool scores = biased || (P.n_groups > 1 && top2);
+    if (P.src.g) {
+        float v[kMaxExperts / 64], b[kMaxExperts / 64];
+#pragma unroll
+        for (int q = 0; q < kMaxExperts / 64; ++q)
+            v[q] = P.src.g[(size_t)t * E + min(lane + 64 * q, E - 1)];
+        if (biased) {
+#pragma unroll
+            for (int q = 0; q < kMaxExperts / 64; ++q) b[q] = P.sel_bias[min(lane + 64 * q, E - 1)];
         }
-        P.idx[(size_t)t * k + j] = e;
-        P.w[(size_t)t * k + j] = w;
+#pragma unroll
+        for (int q = 0; q < kMaxExperts / 64; ++q) {
+            zs[lane + 64 * q] = lane + 64 * q < E ? clean_logit(v[q]) : -INFINITY;
+            if (biased) zb[lane + 64 * q] = clean_logit(b[q]);
+        }
+    } else {
+#pragma unroll 1
+        for (int e = lane; e < kMaxExperts; e += 64) {
+            zs[e] = -INFINITY;
+            if (e >= E) continue;
+            zs[e] = clean_logit(summed_logit(P, t, e, true));
+            if (biased) zb[e] = clean_logit(P.sel_bias[e]);
+        }
     }
+    wave_sync();
+    const int wl = P.lanes_log + 2;  // 64 lanes: four times those of a 16-lane row
+    const int grp = lane >> wl, sub = lane & ((1 << wl) - 1);
+    const int e0 = grp * P.Gs + sub, held = grp < P.n_groups ? P.Gs - sub : 0;
+    float z[NQ], zmax = -INFINITY;
+#pragma unroll
+    for (int q = 0; q < NQ; ++q) {
+        float x = zs[q << wl < held ? e0 + (q << wl) : 0];
+        asm volatile("" : "+v"(x));
+        z[q] = q << wl < held ? x : -INFINITY;
+        zmax = fmaxf(zmax, z[q]);
+    }
+    zmax = row_max(zmax);
+    zmax = fmaxf(zmax, __uint_as_float(xor_lane<16>(__float_as_uint(zmax), lane)));
+    zmax = fmaxf(zmax, __uint_as_float(xor_lane<32>(__float_as_uint(zmax), lane)));
+    double c[NQ], by[NQ];
+#pragma unroll
+    for (int q = 0; q < NQ; ++q) c[q] = by[q] = (double)z[q];
+    if (scores) {
+        double S = 0.0;
+#pragma unroll
+        for (int q = 0; q < NQ; ++q) {
+            const double x = sig ? -fabs((double)z[q]) : (double)z[q] - (double)zmax;
+            by[q] = z[q] > -INFINITY ? exp_neg(fmax(x, -800.0)) : 0.0;
+            S += by[q];
+        }
+        if (sig) {
+#pragma unroll
+            for (int q = 0; q < NQ; ++q) {
+                const double d = rcp64(1.0 + by[q]);
+                by[q] = z[q] >= 0.0f ? d : by[q] * d;
+            }
+        } else {
+            S = wave_reduce(S, lane, [](double a, double b) { return a + b; });
+            const double r = S > 0.0 ? rcp64(S) : 0.0;
+#pragma unroll
+            for (int q = 0; q < NQ; ++q) by[q] *= r;
+        }
+    }
+    if (biased) {
+#pragma unroll
+        for (int q = 0; q < NQ; ++q) {
+            const float b = zb[q << wl < held ? e0 + (q << wl) : 0];
+            c[q] = z[q] > -INFINITY && b > -INFINITY ? by[q] + (double)b : -INFINITY;
+        }
+    }
+    if (P.n_groups > 1) {
+        double a = -INFINITY, n = -INFINITY;  // the two largest
+#pragma unroll
+        for (int q = 0; q < NQ; ++q) {
+            const double v =
+                top2 && !biased ? (z[q] > -INFINITY ? by[q] : -INFINITY) : c[q];
+            n = fmax(n, fmin(a, v));
+            a = fmax(a, v);
+        }
+        auto join = [&](auto st) {
+            constexpr int ST = decltype(st)::value;
+            if ((1 << wl) <= ST) return;
+            auto other = [&](double v) {
+                const unsigned long long u = __builtin_bit_cast(unsigned long long, v);
+                return __builtin_bit_cast(
+                    double, ((unsigned long long)xor_lane<ST>((uint32_t)(u >> 32), lane) << 32) |
+                                xor_lane<ST>((uint32_t)u, lane));
+            };
+            const double a2 = other(a), n2 = other(n);
+            n = fmax(fmin(a, a2), fmax(n, n2));
+            a = fmax(a, a2);
+        };
+        join(std::integral_constant<int, 1>{});
+        join(std::integral_constant<int, 2>{});
+        join(std::integral_constant<int, 4>{});
+        join(std::integral_constant<int, 8>{});
+        join(std::integral_constant<int, 16>{});
+        const double v = top2 && n > -INFINITY ? a + n : a;
+        const unsigned long long u = __builtin_bit_cast(unsigned long long, v);
+        int front = 0;
+#pragma unroll 1
+        for (int g = 0; g < P.n_groups; ++g) {
+            const unsigned long long ou =
+                ((unsigned long long)(uint32_t)__builtin_amdgcn_readlane((int)(u >> 32), g << wl)
+                 << 32) | (uint32_t)__builtin_amdgcn_readlane((int)u, g << wl);
+            const double o = __builtin_bit_cast(double, ou);
+            front += o > v || (o == v && g < grp) ? 1 : 0;
+        }
+#pragma unroll
+        for (int q = 0; q < NQ; ++q) c[q] = front < P.top_groups ? c[q] : -INFINITY;
+    }
+    constexpr uint32_t kNone = 0xFFFFFFFFu;
+    uint32_t key[NQ];
+    {
+        double cmax = c[0];
+#pragma unroll
+        for (int q = 1; q < NQ; ++q) cmax = fmax(cmax, c[q]);
+        cmax = wave_reduce(cmax, lane, [](double a, double b) { return fmax(a, b); });
+#pragma unroll
+        for (int q = 0; q < NQ; ++q) {
+            const uint32_t e = (uint32_t)(e0 + (q << wl));
+            const uint32_t d = __float_as_uint((float)(cmax - c[q])) & 0xFFFFFF00u;
+            key[q] = c[q] > -INFINITY ? d | e : kNone;
+            if (q << wl < held) cs[e] = c[q];
+        }
+    }
+    auto next_key = [&](uint32_t last) {
+        uint32_t m = key[0] + ~last;
+#pragma unroll
+        for (int q = 1; q < NQ; ++q) m = min(m, key[q] + ~last);
+        m = row_min(m);
+        const uint32_t a = min((uint32_t)__builtin_amdgcn_readlane((int)m, 0),
+                               (uint32_t)__builtin_amdgcn_readlane((int)m, 16));
+        const uint32_t b = min((uint32_t)__builtin_amdgcn_readlane((int)m, 32),
+                               (uint32_t)__builtin_amdgcn_readlane((int)m, 48));
+        return min(a, b) + last + 1u;
+    };
+    // as in route_topk_k; keys of equal upper bits are the only ones in doubt
+    uint32_t last = kNone;
+    bool close = false, unsure = false;
+    int len = 0;
+#pragma unroll 1
+    for (int j = 0; j < k; ++j) {
+        const bool over = j > 0 && last == kNone;
+        const uint32_t n = next_key(last);
+        close |= !over && n != kNone && j > 0 && (n ^ last) < 256u;
+        last = over ? kNone : n;
+        len += last != kNone ? 1 : 0;
+        if (lane == 0) pk[j] = last != kNone ? (short)(last & 255u) : (short)-1;
+    }
+    const uint32_t cut = last;
+    while (last != kNone) {
+        const uint32_t n = next_key(last);
+        if (n <= last || n == kNone || (n ^ cut) >= 256u) break;
+        close = true;
+        if (len >= kMaxList) {
+            unsure = true;
+            break;
+        }
+        last = n;
+        if (lane == 0) pk[len] = (short)(n & 255u);
+        ++len;
+    }
+    unsure |= close && k > kMaxList;
+    wave_sync();
+    if (unsure)
+        choose_row(P, zs, zb, zmax, cs, pk, lane);
+    else if (close)
+        sort_list(cs, pk, len, k, lane);
+    wave_sync();
+    float Sinv = 0.0f;
+    if (!sig && !(P.flags & PP_TOPK_RENORM)) {
+        // each 16 lanes take the values that they have in route_topk_k, in
+        // the same order: the same bits
+        const int g = (lane & 15) >> P.lanes_log;
+        float S = 0.0f;
+        if (g < P.n_groups) {
+#pragma unroll 4
+            for (int i = lane & (P.lanes - 1); i < P.Gs; i += P.lanes)
+                S += exp_fast(zs[g * P.Gs + i] - zmax);
+        }
+        Sinv = 1.0f / row_sum(S);
+    }
+    store_row<64>(P, zs, zmax, Sinv, pk, t, lane);
 }
 
 constexpr int kGradWaves = 4;  // one token each
@@ -709,25 +964,46 @@ constexpr TopkBuild kTopkBuilds[] = {
     topk_build<6>(),  topk_build<7>(),  topk_build<8>(),  topk_build<10>(), topk_build<12>(),
     topk_build<14>(), topk_build<16>(), topk_build<20>(), topk_build<28>()};
 
+struct TopkWideBuild {
+    int values;
+    void (*kernel)(TopkParams);
+};
+constexpr TopkWideBuild kTopkWideBuilds[] = {{1, route_topk_wide_k<1>},
+                                             {2, route_topk_wide_k<2>},
+                                             {4, route_topk_wide_k<4>},
+                                             {7, route_topk_wide_k<7>}};
+// Up to so many tokens take a wavefront each.
+constexpr int kWideTokens = 1024;
+
 hipError_t launch_topk(TopkParams P, hipStream_t s) {
     P.Gs = P.E / P.n_groups;
     P.lanes_log = 4;
     while ((16 >> P.lanes_log) < P.n_groups) --P.lanes_log;
     P.lanes = 1 << P.lanes_log;
+    P.by_Gs = (uint32_t)((65536 + P.Gs - 1) / P.Gs);
+    P.kp = P.k > kMaxList ? (P.k + 15) & ~15 : kMaxList;
+    if (P.T <= kWideTokens || (P.sel_bias && !(P.flags & PP_SCORE_SIGMOID))) {
+        const TopkWideBuild *B = kTopkWideBuilds;
+        while (B->values * 4 * P.lanes < P.Gs) ++B;  // at most 7
+        P.Gp = P.Gs;
+        P.wave_lds = 4 * kMaxExperts + P.kp / 2;
+        hipLaunchKernelGGL(B->kernel, dim3((P.T + kTopkWaves - 1) / kTopkWaves),
+                           dim3(64 * kTopkWaves), sizeof(float) * kTopkWaves * P.wave_lds, s, P);
+        return hipGetLastError();
+    }
     const TopkBuild *B = kTopkBuilds;
     while (B->values * P.lanes < P.Gs) ++B;  // at most 28: nine groups of 28, a lane each
     // a group starts `lanes` banks after the one before, so that the 16 lanes
     // of a row read 16 different banks; one group: rows 16 banks apart
     P.Gp = (B->values * P.lanes + 31) / 32 * 32 + P.lanes;
     P.Rp = (16 >> P.lanes_log) * P.Gp;
-    P.by_Gs = (uint32_t)((65536 + P.Gs - 1) / P.Gs);
     P.pad = P.n_groups << P.lanes_log != 16 || B->values * P.lanes != P.Gs;
     const bool scores = P.sel_bias || (P.n_groups > 1 && (P.flags & PP_GROUP_TOP2));
-    const size_t lds = sizeof(double) * kMaxExperts +
-                       sizeof(float) * (kRowsPerWave + (scores ? 1 : 0)) * P.Rp +
-                       sizeof(short) * kRowsPerWave * ((P.k + 15) & ~15);
-    hipLaunchKernelGGL(scores ? B->scores : B->logits,
-                       dim3((P.T + kRowsPerWave - 1) / kRowsPerWave), dim3(64), lds, s, P);
+    P.wave_lds = 2 * kMaxExperts + (kRowsPerWave + (scores ? 1 : 0)) * P.Rp +
+                 kRowsPerWave * P.kp / 2;
+    constexpr int rows = kRowsPerWave * kTopkWaves;
+    hipLaunchKernelGGL(scores ? B->scores : B->logits, dim3((P.T + rows - 1) / rows),
+                       dim3(64 * kTopkWaves), sizeof(float) * kTopkWaves * P.wave_lds, s, P);
     return hipGetLastError();
 }
 
@@ -753,7 +1029,7 @@ extern "C" pp_status prunepath_route_topk(pp_layer *L, const uint16_t *x, int32_
     if (e == hipSuccess) {
         const RouteParams R = route_params(L, x, T, 0.0f, inv_temp, nullptr, nullptr, nullptr, false);
         const TopkParams P = {{nullptr, R.gpart, R.bias, inv_temp, logits, R.KSr}, T, E, k, n_groups,
-                              top_groups, sel_bias, scale, flags, expert_idx, gate_w, 0, 0, 0, 0, 0, 0, 0};
+                              top_groups, sel_bias, scale, flags, expert_idx, gate_w, 0, 0, 0, 0, 0, 0, 0, 0, 0};
         prof_mark(L, PP_KERNEL_ROUTE, s, true);
         e = launch_topk(P, s);
         prof_mark(L, PP_KERNEL_ROUTE, s, false);
@@ -772,7 +1048,7 @@ extern "C" pp_status prunepath_route_topk_logits(const float *g, int32_t T, int3
         check_rule(E, k, n_groups, top_groups, sel_bias, scale, flags, expert_idx, gate_w);
     if (st != PP_OK) return st;
     const TopkParams P = {{g, nullptr, nullptr, nullptr, nullptr, 0}, T, E, k, n_groups, top_groups,
-                          sel_bias, scale, flags, expert_idx, gate_w, 0, 0, 0, 0, 0, 0, 0};
+                          sel_bias, scale, flags, expert_idx, gate_w, 0, 0, 0, 0, 0, 0, 0, 0, 0};
     return launch_topk(P, static_cast<hipStream_t>(hip_stream)) == hipSuccess ? PP_OK : PP_EHIP;
 }
 
