@@ -831,19 +831,6 @@ __global__ __launch_bounds__(64 * kTopkWaves) void route_topk_wide_k(TopkParams 
     store_row<64>(P, zs, zmax, Sinv, pk, t, lane);
 }
 
-constexpr int kGradWaves = 4;  // one token each
-
-__device__ __forceinline__ float wave_max_f32(float v) {
-#pragma unroll
-    for (int st = 1; st < 64; st <<= 1) v = fmaxf(v, __shfl_xor(v, st, 64));
-    return v;
-}
-__device__ __forceinline__ float wave_sum_f32(float v) {
-#pragma unroll
-    for (int st = 1; st < 64; st <<= 1) v += __shfl_xor(v, st, 64);
-    return v;
-}
-
 struct TopkGradParams {
     const float *g;
     int T, E, k;
@@ -854,83 +841,163 @@ struct TopkGradParams {
     float *dg;
 };
 
-// dL/dg of one token per wavefront, the chosen experts held fixed.  With
-// a_j = dw_j over the slots that name an expert, q_j = w_j / scale:
-//   softmax            dg_e = scale p_e ([e chosen] a_e - sum_j p_j a_j)
-//   sigmoid            dg_e = scale s_e (1 - s_e) a_e
-//   renormalised, D = sum_j q_j a_j:
-//   softmax            dg_e = scale q_e (a_e - D)
-//   sigmoid            dg_e = scale q_e (1 - s_e) (a_e - D)
-__global__ __launch_bounds__(64 * kGradWaves) void route_topk_grad_k(TopkGradParams P) {
-    const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6;
-    const int t = blockIdx.x * kGradWaves + wv;
-    if (t >= P.T) return;
+// dL/dg, the chosen experts held fixed.  With a_j = dw_j over the slots that
+// name an expert, q_j = w_j / scale and D = sum_j q_j a_j:
+//   softmax                 dg_e = scale p_e ([e chosen] a_e - D)
+//   sigmoid                 dg_e = scale s_e (1 - s_e) a_e
+//   renormalised softmax    dg_e = scale q_e (a_e - D)
+//   renormalised sigmoid    dg_e = scale q_e (1 - s_e) (a_e - D)
+// Bound by memory (dg is written whole).  A token takes 16 lanes: lane c has
+// slots c, c + 16, ... and columns c, c + 16, ... (NQ of them); the slots'
+// values meet the columns in LDS.  ROW: plain softmax, whose gradient reaches
+// every expert and needs the whole row; else only the slots' logits are read.
+template <int NQ, bool ROW>
+__global__ __launch_bounds__(64 * kTopkWaves) void route_topk_grad_k(TopkGradParams P) {
+    // rows start 16 (or 48) banks apart
+    constexpr int kStride = 16 * (NQ % 2 ? NQ : NQ + 1);
+    __shared__ float acc_lds[kTopkWaves][kRowsPerWave * kStride];
+    __shared__ short own_lds[kTopkWaves][kRowsPerWave * kStride];
+    const int wv = threadIdx.x >> 6, lane = threadIdx.x & 63, c16 = lane & 15, rr = lane >> 4;
+    const int t0 = (int)(blockIdx.x * kTopkWaves + wv) * kRowsPerWave;
+    if (t0 >= P.T) return;
+    float *const acc = acc_lds[wv] + rr * kStride;
+    short *const own = own_lds[wv] + rr * kStride;
     const bool sig = (P.flags & PP_SCORE_SIGMOID) != 0;
     const bool renorm = (P.flags & PP_TOPK_RENORM) != 0;
-    const int E = P.E;
-    constexpr int NQ = kMaxExperts / 64;
-    const float *row = P.g + (size_t)t * E;
-    const int32_t *idx = P.idx + (size_t)t * P.k;
-    const float *dw = P.dw + (size_t)t * P.k;
-    float z[NQ], p[NQ], acc[NQ];
-    float zmax = -INFINITY;
+    const int E = P.E, k = P.k, t = t0 + rr, tc = min(t, P.T - 1);
+    const float *const row = P.g + (size_t)tc * E;
+    const int32_t *const idx = P.idx + (size_t)tc * k;
+    const float *const dw = P.dw + (size_t)tc * k;
+    struct Slot {
+        int e;      // -1: empty
+        float a, z;
+    };
+    auto load = [&](int j) {
+        Slot s = {-1, 0.0f, -INFINITY};
+        if (j >= k) return s;
+        const int e = idx[j];
+        const float a = dw[j];
+        if ((unsigned)e >= (unsigned)E) return s;
+        s.z = clean_logit(row[e]);
+        if (s.z > -INFINITY) s.e = e, s.a = a;
+        return s;
+    };
+    const Slot first = load(c16);
+    auto slot = [&](int j) { return j < 16 ? first : load(j); };
+    float p[NQ], zmax = -INFINITY, Sinv = 0.0f;
+    if constexpr (ROW) {
 #pragma unroll
-    for (int q = 0; q < NQ; ++q) {
-        const int e = lane + 64 * q;
-        z[q] = e < E ? clean_logit(row[e]) : -INFINITY;
-        zmax = fmaxf(zmax, z[q]);
-        acc[q] = 0.0f;
-    }
-    zmax = wave_max_f32(zmax);
-    float S = 0.0f;
+        for (int q = 0; q < NQ; ++q) p[q] = row[min(c16 + 16 * q, E - 1)];
 #pragma unroll
-    for (int q = 0; q < NQ; ++q) {
-        p[q] = z[q] > -INFINITY ? expf(z[q] - zmax) : 0.0f;
-        S += p[q];
+        for (int q = 0; q < NQ; ++q) {
+            p[q] = c16 + 16 * q < E ? clean_logit(p[q]) : -INFINITY;
+            zmax = fmaxf(zmax, p[q]);
+        }
+        zmax = row_max(zmax);
+        float S = 0.0f;
+#pragma unroll
+        for (int q = 0; q < NQ; ++q) {
+            p[q] = p[q] > -INFINITY ? exp_fast(p[q] - zmax) : 0.0f;
+            S += p[q];
+        }
+        S = row_sum(S);
+        Sinv = S > 0.0f ? 1.0f / S : 0.0f;
     }
-    S = wave_sum_f32(S);
+#pragma unroll
+    for (int q = 0; q < NQ; ++q) acc[c16 + 16 * q] = 0.0f;
     // scores of the slots, relative to the largest where they are renormalised
-    float m = -INFINITY;
-    for (int j = 0; j < P.k; ++j) {
-        const int e = idx[j];
-        if ((unsigned)e < (unsigned)E) m = fmaxf(m, clean_logit(row[e]));
+    float m = ROW ? zmax : 0.0f, inv = ROW ? Sinv : 1.0f, D = 0.0f;
+    auto score = [&](const Slot &s) { return sig ? rel_sigmoid(s.z, m) : expf(s.z - m); };
+    if (renorm) {
+        m = -INFINITY;
+        for (int j = c16; j < k; j += 16) m = fmaxf(m, slot(j).z);
+        m = row_max(m);
+        if (sig) m = fminf(m, 0.0f);
     }
-    if (sig) m = renorm ? fminf(m, 0.0f) : 0.0f;
-    if (!sig && !renorm) m = zmax;
-    float tot = 0.0f, D = 0.0f;
-    for (int j = 0; j < P.k; ++j) {
-        const int e = idx[j];
-        if ((unsigned)e >= (unsigned)E) continue;
-        const float x = clean_logit(row[e]);
-        if (!(x > -INFINITY)) continue;
-        const float sc = sig ? rel_sigmoid(x, m) : expf(x - m);
-        tot += sc;
-        D += sc * dw[j];
+    if (renorm || ROW) {
+        float tot = 0.0f;
+        for (int j = c16; j < k; j += 16) {
+            const Slot s = slot(j);
+            if (s.e < 0) continue;
+            const float q = score(s);
+            tot += q;
+            D += q * s.a;
+        }
+        if (renorm) {
+            tot = row_sum(tot);
+            inv = tot > 0.0f ? 1.0f / tot : 0.0f;
+        }
+        D = row_sum(D) * inv;
     }
-    if (!sig && !renorm) tot = S;
-    const float inv = sig && !renorm ? 1.0f : (tot > 0.0f ? 1.0f / tot : 0.0f);
-    D = sig && !renorm ? 0.0f : D * inv;
-    for (int j = 0; j < P.k; ++j) {
-        const int e = idx[j];
-        if ((unsigned)e >= (unsigned)E) continue;
-        const float x = clean_logit(row[e]);
-        if (!(x > -INFINITY)) continue;
-        const float sc = sig ? rel_sigmoid(x, m) : expf(x - m);
-        float v = sc * inv * (renorm ? dw[j] - D : dw[j]);
-        if (sig) v *= rel_sigmoid(-x, 0.0f);
+    // whether a token names an expert twice
+    bool twice = false;
+    for (int j = c16; j < k; j += 16) {
+        const Slot s = slot(j);
+        if (s.e >= 0) own[s.e] = (short)j;
+    }
+    wave_sync();
+    for (int j = c16; j < k; j += 16) {
+        const Slot s = slot(j);
+        if (s.e >= 0) twice |= own[s.e] != (short)j;
+    }
+    const bool add = __ballot(twice) != 0ull;
+    for (int j0 = 0; j0 < k; j0 += 16) {
+        const Slot s = slot(j0 + c16);
+        float v = 0.0f;
+        if (s.e >= 0) {
+            v = score(s) * inv * (renorm ? s.a - D : s.a);
+            if (sig) v *= rel_sigmoid(-s.z, 0.0f);
+        }
+        if (!add) {
+            if (s.e >= 0) acc[s.e] = v;
+        } else {
+            for (int j = 0; j < 16; ++j) {  // in slot order
+                if (c16 == j && s.e >= 0) acc[s.e] += v;
+                wave_sync();
+            }
+        }
+    }
+    wave_sync();
+    if (t >= P.T) return;
+    float *const out = P.dg + (size_t)t * E;
+    float old[NQ];
+    if (P.flags & PP_GRAD_ADD) {
 #pragma unroll
-        for (int q = 0; q < NQ; ++q) acc[q] += lane + 64 * q == e ? v : 0.0f;
+        for (int q = 0; q < NQ; ++q) old[q] = out[min(c16 + 16 * q, E - 1)];
+    } else {
+#pragma unroll
+        for (int q = 0; q < NQ; ++q) old[q] = 0.0f;
     }
 #pragma unroll
     for (int q = 0; q < NQ; ++q) {
-        const int e = lane + 64 * q;
-        if (e >= E) continue;
-        float v = acc[q];
-        if (!sig && !renorm) v -= p[q] * inv * D;
-        float *out = P.dg + (size_t)t * E + e;
-        v *= P.scale;
-        *out = (P.flags & PP_GRAD_ADD) ? *out + v : v;
+        float v = acc[c16 + 16 * q];
+        if constexpr (ROW) v -= p[q] * inv * D;
+        if (c16 + 16 * q < E) out[c16 + 16 * q] = old[q] + P.scale * v;
     }
+}
+
+template <int NQ>
+void launch_topk_grad_nq(const TopkGradParams &P, hipStream_t s) {
+    constexpr int rows = kRowsPerWave * kTopkWaves;
+    const dim3 grid((P.T + rows - 1) / rows), block(64 * kTopkWaves);
+    if (P.flags & (PP_SCORE_SIGMOID | PP_TOPK_RENORM))
+        hipLaunchKernelGGL((route_topk_grad_k<NQ, false>), grid, block, 0, s, P);
+    else
+        hipLaunchKernelGGL((route_topk_grad_k<NQ, true>), grid, block, 0, s, P);
+}
+
+void launch_topk_grad(const TopkGradParams &P, hipStream_t s) {
+    const int need = (P.E + 15) / 16;
+    if (need <= 2)
+        launch_topk_grad_nq<2>(P, s);
+    else if (need <= 4)
+        launch_topk_grad_nq<4>(P, s);
+    else if (need <= 7)
+        launch_topk_grad_nq<7>(P, s);
+    else if (need <= 10)
+        launch_topk_grad_nq<10>(P, s);
+    else
+        launch_topk_grad_nq<16>(P, s);
 }
 
 constexpr uint32_t kRuleFlags = PP_SCORE_SIGMOID | PP_TOPK_RENORM | PP_GROUP_TOP2;
@@ -1065,7 +1132,6 @@ extern "C" pp_status prunepath_route_topk_grad(const float *g, int32_t T, int32_
     if (flags & ~(kRuleFlags | PP_GRAD_ADD)) return PP_EINVAL;
     if (!(fabsf(scale) <= 3.0e38f)) return PP_EINVAL;
     const TopkGradParams P = {g, T, E, k, expert_idx, dgate_w, scale, flags, dg};
-    hipLaunchKernelGGL(route_topk_grad_k, dim3((T + kGradWaves - 1) / kGradWaves),
-                       dim3(64 * kGradWaves), 0, static_cast<hipStream_t>(hip_stream), P);
+    launch_topk_grad(P, static_cast<hipStream_t>(hip_stream));
     return hipGetLastError() == hipSuccess ? PP_OK : PP_EHIP;
 }
