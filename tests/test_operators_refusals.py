@@ -6,6 +6,7 @@ import pytest
 
 import paper_2605_28283_amd as pp
 from oracle import operators as op
+from paper_2605_28283_amd.stack import DecodeStack
 
 INF, NAN = float("inf"), float("nan")
 MANY = pp.PP_SCORE_SIGMOID | pp.PP_TOPK_RENORM | pp.PP_GROUP_TOP2
@@ -88,6 +89,17 @@ def test_layernorm_grad_workspace():
         assert size(T, d) > 0 and size(T, d) % 4 == 0
     for T, d in ((0, 8), (8, 0), (-1, 8), ((1 << 20) + 1, 8), (8, 65537)):
         assert size(T, d) == 0
+
+
+def test_stack_refuses():
+    with pytest.raises(ValueError):
+        DecodeStack([1, 2], 64, 2, 1, 0.5, norms=[(None, None)])
+    with pytest.raises(ValueError):
+        DecodeStack([1, 2], 64, 2, 1, 0.5, topk=dict(k=1, groups=2))
+    with pytest.raises(ValueError):
+        DecodeStack([1, 2], 64, 2, 1, 0.5, topk=dict(n_groups=2))
+    with pytest.raises(ValueError):
+        DecodeStack([1, 2], 64, 2, 1, 0.5, topk=dict(k=1, sel_bias=[None]))
 
 
 # ------------------------------------------------------------------ the fp64 forms
