@@ -72,8 +72,21 @@ struct TopkParams {
 
 // NaN and -inf to -inf, +inf to the largest float.
 __device__ __forceinline__ float clean_logit(float z) {
-    return z > -INFINITY ? fminf(z, kFltMax) : -INFINITY;
+    return fminf(fmaxf(z, -INFINITY), kFltMax);
 }
+// Maximum and minimum of numbers without the quieting of NaNs that fmaxf and
+// fminf are compiled to: medians with an infinity, which must not be known as
+// one (else they are turned back).
+struct NumExtremes {
+    float inf = INFINITY;
+    __device__ __forceinline__ NumExtremes() { asm("" : "+s"(inf)); }
+    __device__ __forceinline__ float max(float a, float b) const {
+        return __builtin_amdgcn_fmed3f(a, b, inf);
+    }
+    __device__ __forceinline__ float min(float a, float b) const {
+        return __builtin_amdgcn_fmed3f(a, b, -inf);
+    }
+};
 
 // ---- the 16 lanes of a DPP row
 template <int CTRL>
@@ -101,11 +114,15 @@ __device__ __forceinline__ V row_reduce(V v, F f) {
     v = f(v, row_lane<kX4>(v));
     return f(v, row_lane<kX8>(v));
 }
+// Floats in the order of signed integers (its own inverse).
+__device__ __forceinline__ int ordered_bits(int u) { return u ^ ((u >> 31) & 0x7FFFFFFF); }
 __device__ __forceinline__ float row_max(float v) {
-    return row_reduce(v, [](float a, float b) { return fmaxf(a, b); });
-}
-__device__ __forceinline__ double row_max(double v) {
-    return row_reduce(v, [](double a, double b) { return fmax(a, b); });
+    int m = ordered_bits(__float_as_int(v));
+    m = max(m, (int)row_u32<kX1>((uint32_t)m));
+    m = max(m, (int)row_u32<kX2>((uint32_t)m));
+    m = max(m, (int)row_u32<kX4>((uint32_t)m));
+    m = max(m, (int)row_u32<kX8>((uint32_t)m));
+    return __int_as_float(ordered_bits(m));
 }
 template <typename V>
 __device__ __forceinline__ V row_sum(V v) {
@@ -173,13 +190,12 @@ __device__ __forceinline__ float rel_sigmoid(float z, float m) {
 __device__ __forceinline__ float exp_fast(float x) {
     return __builtin_amdgcn_exp2f(x * 1.44269504088896341f);
 }
-// sigmoid(z) within 4e-7: e = e^-|z| is off by e (|z| 2^-23 + 2^-22) < 2.9e-7
-// (the product with log2 e, the exponential), which counts 1 / (1 + e)^2 of
-// that; 1 + e, its reciprocal and e r add 2^-24 + 2^-23 + 2^-25.
+// sigmoid(z) within 4e-7: e = e^-z is off by e (|z| 2^-23 + 2^-22) (the product
+// with log2 e, the exponential), of which s^2 counts, at most 2.9e-7 for
+// either sign of z; 1 + e and its reciprocal add (2^-24 + 2^-23) s.
 constexpr float kScoreErr = 6e-7f;
 __device__ __forceinline__ float sigmoid_fast(float z) {
-    const float e = exp_fast(-fabsf(z)), r = __builtin_amdgcn_rcpf(1.0f + e);
-    return z >= 0.0f ? r : e * r;
+    return __builtin_amdgcn_rcpf(1.0f + exp_fast(-z));
 }
 
 // Largest and smallest over the wavefront, sum over it.
@@ -399,7 +415,8 @@ __global__ __launch_bounds__(64 * kTopkWaves) void route_topk_k(TopkParams P) {
     short *const pk = reinterpret_cast<short *>(zb + (SCORES ? P.Rp : 0));  // [4][kp]
     const int lane = threadIdx.x & 63, c16 = lane & 15, rr = lane >> 4;
     const int E = P.E, k = P.k;
-    const int t0 = (int)(blockIdx.x * kTopkWaves + (threadIdx.x >> 6)) * kRowsPerWave;
+    const int t0 = __builtin_amdgcn_readfirstlane(
+        (int)(blockIdx.x * kTopkWaves + (threadIdx.x >> 6)) * kRowsPerWave);
     if (t0 >= P.T) return;
     const bool sig = (P.flags & PP_SCORE_SIGMOID) != 0;
     const bool top2 = (P.flags & PP_GROUP_TOP2) != 0;
@@ -413,6 +430,7 @@ __global__ __launch_bounds__(64 * kTopkWaves) void route_topk_k(TopkParams P) {
             reinterpret_cast<float4 *>(zs)[i] =
                 make_float4(-INFINITY, -INFINITY, -INFINITY, -INFINITY);
     }
+    float big = 0.0f;  // largest |bias|
     // the bias and four rows to LDS, every load issued first
     if (P.src.g) {
         float v[kRowsPerWave + 1][NE];
@@ -433,13 +451,21 @@ __global__ __launch_bounds__(64 * kTopkWaves) void route_topk_k(TopkParams P) {
             const int at = topk_place(P, e);
 #pragma unroll
             for (int r = 0; r < kRowsPerWave; ++r) zs[r * P.Rp + at] = clean_logit(v[r][q]);
-            if (biased) zb[at] = clean_logit(v[kRowsPerWave][q]);
+            if (biased) {
+                const float b = clean_logit(v[kRowsPerWave][q]);
+                zb[at] = b;
+                big = b > -INFINITY ? fmaxf(big, fabsf(b)) : big;
+            }
         }
     } else {
 #pragma unroll 1
         for (int e = lane; e < E; e += 64) {
             const int at = topk_place(P, e);
-            if (biased) zb[at] = clean_logit(P.sel_bias[e]);
+            if (biased) {
+                const float b = clean_logit(P.sel_bias[e]);
+                zb[at] = b;
+                big = b > -INFINITY ? fmaxf(big, fabsf(b)) : big;
+            }
 #pragma unroll 1
             for (int r = 0; r < kRowsPerWave; ++r)
                 zs[r * P.Rp + at] =
@@ -451,55 +477,64 @@ __global__ __launch_bounds__(64 * kTopkWaves) void route_topk_k(TopkParams P) {
     // the lane's group and its first value
     const int grp = c16 >> P.lanes_log, sub = c16 & (P.lanes - 1);
     const float *const mz = zr + grp * P.Gp + sub;
-    float c[NQ], zmax = -INFINITY;
+    const NumExtremes num;
+    float c[NQ], zmax = 0.0f;
 #pragma unroll
-    for (int q = 0; q < NQ; ++q) {
-        c[q] = mz[q * P.lanes];
-        zmax = fmaxf(zmax, c[q]);
-    }
-    zmax = row_max(zmax);
-    // 1 / sum of e^(z - zmax), where softmax weights are wanted as they are
+    for (int q = 0; q < NQ; ++q) c[q] = mz[q * P.lanes];
+    // softmax: the row's largest logit, and 1 / sum of e^(z - zmax) where
+    // weights are wanted as they are
     float Sinv = 0.0f;
-    if (!sig && !renorm) {
-        float S = 0.0f;
+    if (!sig) {
+        zmax = c[0];
 #pragma unroll
-        for (int q = 0; q < NQ; ++q) S += exp_fast(c[q] - zmax);
-        Sinv = 1.0f / row_sum(S);  // a row of no experts has no weights
+        for (int q = 1; q < NQ; ++q) zmax = num.max(zmax, c[q]);
+        zmax = row_max(zmax);
+        if (!renorm) {
+            float S = 0.0f;
+#pragma unroll
+            for (int q = 0; q < NQ; ++q) S += exp_fast(c[q] - zmax);
+            Sinv = 1.0f / row_sum(S);  // a row of no experts has no weights
+        }
     }
     bool unsure = false;  // whether 32 bits do not make the choice
     float err = 0.0f;     // of c
     if constexpr (SCORES) {
-        float big = 0.0f;
-        const float *const mb = zb + grp * P.Gp + sub;
-        {
+        // the score's error and the rounding of the sum with the bias
+        if (biased) {
 #pragma unroll
-            for (int q = 0; q < NQ; ++q) {
-                float v = sig ? sigmoid_fast(c[q]) : exp_fast(c[q] - zmax);
-                float b = 0.0f;
-                if (biased) {
-                    b = mb[q * P.lanes];
-                    v += b;
-                }
-                // computed for every lane, not in a branch of its own
-                asm volatile("" : "+v"(v));
-                c[q] = fminf(c[q], b) > -INFINITY ? v : -INFINITY;
-                big = fmaxf(big, c[q] > -INFINITY ? fabsf(v) : 0.0f);
-            }
-            // the score's error and the rounding of the sum with the bias
-            err = kScoreErr + row_max(big) * 2.4e-7f;
+            for (int st = 1; st < 64; st <<= 1)
+                big = fmaxf(big, __uint_as_float(xor_lane_rt(__float_as_uint(big), st, lane)));
         }
+        err = kScoreErr + (1.0f + big) * 2.4e-7f;
+        // (an expert that takes no part has a score of 0 here)
+        float s[NQ];
+        if (sig) {
+#pragma unroll
+            for (int q = 0; q < NQ; ++q) s[q] = sigmoid_fast(c[q]);
+        } else {
+#pragma unroll
+            for (int q = 0; q < NQ; ++q) s[q] = exp_fast(c[q] - zmax);
+        }
+        if (biased) {
+            const float *const mb = zb + grp * P.Gp + sub;
+#pragma unroll
+            for (int q = 0; q < NQ; ++q) s[q] += mb[q * P.lanes];  // -inf: takes no part
+        }
+#pragma unroll
+        for (int q = 0; q < NQ; ++q) c[q] = c[q] > -INFINITY ? s[q] : -INFINITY;
     }
     // the groups that stay
+    bool out = false;
     if (P.n_groups > 1) {
-        float a = -INFINITY, n = -INFINITY;  // the two largest
+        float a = c[0], n = -INFINITY;  // the two largest
 #pragma unroll
-        for (int q = 0; q < NQ; ++q) {
+        for (int q = 1; q < NQ; ++q) {
             n = __builtin_amdgcn_fmed3f(n, a, c[q]);  // n <= a: the middle one
-            a = fmaxf(a, c[q]);
+            a = num.max(a, c[q]);
         }
         auto join = [&](float a2, float n2) {
-            n = fmaxf(fminf(a, a2), fmaxf(n, n2));
-            a = fmaxf(a, a2);
+            n = num.max(num.min(a, a2), num.max(n, n2));
+            a = num.max(a, a2);
         };
         if (P.lanes > 1) join(row_lane<kX1>(a), row_lane<kX1>(n));
         if (P.lanes > 2) join(row_lane<kX2>(a), row_lane<kX2>(n));
@@ -510,44 +545,40 @@ __global__ __launch_bounds__(64 * kTopkWaves) void route_topk_k(TopkParams P) {
         const float off = SCORES ? 3.0f * err : 0.0f;
         int front = 0, near = 0;
         each_rotation([&](auto ctrl) {
-            constexpr int R = decltype(ctrl)::value;
+            constexpr int R = decltype(ctrl)::value & 15;
             if ((R & (P.lanes - 1)) != 0) return;  // from group to group
-            const float o = row_lane<R>(v);
+            const float o = row_lane<decltype(ctrl)::value>(v);
             if constexpr (SCORES) {
                 front += o > v + off ? 1 : 0;
                 near += o >= v - off ? 1 : 0;
             } else {
-                // rotated by R: lane c reads lane c + 16 - R (or c - R)
-                const bool before = (int)row_u32<R>((uint32_t)grp) < grp;
+                const bool before = c16 >= R;  // lane c reads lane c - R, or c - R + 16
                 front += o > v || (o == v && before) ? 1 : 0;
             }
         });
         if (SCORES)
             unsure |= v > -INFINITY && front < P.top_groups && near >= P.top_groups;
-        const bool out = front >= P.top_groups;
-#pragma unroll
-        for (int q = 0; q < NQ; ++q) c[q] = out ? -INFINITY : c[q];
+        out = front >= P.top_groups;
     }
     if (SCORES && !biased) {  // then experts are in the order of the logits
         err = 0.0f;
 #pragma unroll
-        for (int q = 0; q < NQ; ++q) {
-            const float z = mz[q * P.lanes];
-            c[q] = c[q] > -INFINITY ? z : -INFINITY;
-        }
+        for (int q = 0; q < NQ; ++q) c[q] = mz[q * P.lanes];
     }
-    constexpr uint32_t kNone = 0xFFFFFFFFu;
+    // Keys: half the distance (which no two floats overflow) from the largest
+    // c of the groups that stay; infinite for what is not there.
+    constexpr uint32_t kNone = 0xFFFFFFFFu, kFirstNone = 0x7F800000u;
     uint32_t key[NQ];
     {
         float cmax = c[0];
 #pragma unroll
-        for (int q = 1; q < NQ; ++q) cmax = fmaxf(cmax, c[q]);
-        cmax = row_max(cmax);
+        for (int q = 1; q < NQ; ++q) cmax = num.max(cmax, c[q]);
+        const float half = 0.5f * row_max(out ? -INFINITY : cmax);
+        const float from = out ? INFINITY : half;
         uint32_t e = (uint32_t)(grp * P.Gs + sub);
 #pragma unroll
         for (int q = 0; q < NQ; ++q) {
-            const uint32_t d = __float_as_uint(cmax - c[q]) & 0xFFFFFF00u;
-            key[q] = c[q] > -INFINITY ? d | e : kNone;
+            key[q] = (__float_as_uint(fmaf(c[q], -0.5f, from)) & 0xFFFFFF00u) | e;
             e += (uint32_t)P.lanes;
         }
     }
@@ -559,44 +590,42 @@ __global__ __launch_bounds__(64 * kTopkWaves) void route_topk_k(TopkParams P) {
         for (int q = 1; q < NQ; ++q) m = min(m, key[q] + ~last);
         return row_min(m) + last + 1u;
     };
-    // A key's distance from the largest c, and up to which one an entry may
-    // belong in front of it: 2^-15 of each was cut off, and c is off by err.
+    // A key's distance, and up to which one an entry may belong in front of
+    // it: 2^-15 of each was cut off, and c is off by err (halved like it).
     auto distance = [](uint32_t v) { return __uint_as_float(v & 0xFFFFFF00u); };
-    auto reach = [&](uint32_t v) { return distance(v) * 1.0001f + 2.0f * err; };
     uint32_t last = kNone;
+    float reach = 0.0f;
     bool close = false;  // whether the list's order may not be that of c
+    bool more = true;    // whether the list goes on
     int len = 0;         // of the row's list
 #pragma unroll 1
     for (int j = 0; j < k; ++j) {
-        // a list that has ended stays at kNone: the subtraction would wrap
-        const bool over = j > 0 && last == kNone;
         const uint32_t n = next_key(last);
-        close |= !over && n != kNone && j > 0 && distance(n) <= reach(last);
-        last = over ? kNone : n;
-        len += last != kNone ? 1 : 0;
-        if (c16 == 0) pk[rr * kp + j] = last != kNone ? (short)(last & 255u) : (short)-1;
+        more = more && n < kFirstNone;
+        const float d = distance(n);
+        close |= more && j > 0 && d <= reach;
+        reach = fmaf(d, 1.0001f, err);
+        last = n;  // past the list's end: not used any more
+        len += more ? 1 : 0;
+        if (c16 == 0) pk[rr * kp + j] = more ? (short)(n & 255u) : (short)-1;
     }
     // entries past the cut that may belong in front of it
-    {
-        const float cut = reach(last);
-        bool more = last != kNone;
-        for (int m = k;; ++m) {
-            const uint32_t n = next_key(last);
-            more = more && n > last && n != kNone && distance(n) <= cut;
-            if (__ballot(more) == 0ull) break;
-            close |= more;
-            if (m >= kMaxList) {
-                unsure |= more;
-                break;
-            }
-            last = more ? n : last;
-            if (more) {
-                if (c16 == 0) pk[rr * kp + m] = (short)(n & 255u);
-                ++len;
-            }
+    for (int m = k;; ++m) {
+        const uint32_t n = next_key(last);
+        more = more && n > last && n < kFirstNone && distance(n) <= reach;
+        if (__ballot(more) == 0ull) break;
+        close |= more;
+        if (m >= kMaxList) {
+            unsure |= more;
+            break;
         }
-        unsure |= close && k > kMaxList;
+        if (more) {
+            last = n;
+            if (c16 == 0) pk[rr * kp + m] = (short)(n & 255u);
+            ++len;
+        }
     }
+    unsure |= close && k > kMaxList;
     wave_sync();
     // rows whose list is put in order by c in 64 bits
     const unsigned long long sort = __ballot(close && !unsure);
