@@ -256,6 +256,67 @@ __device__ __forceinline__ int topk_place(const TopkParams &P, int e) {
     return g * P.Gp + e - g * P.Gs;
 }
 
+// With the groups spread over 64 lanes (group lane >> (lanes_log + 2)): how
+// many groups are in front of the lane's, whose lanes hold its values' two
+// largest (a, n) among them.
+__device__ __forceinline__ int groups_in_front(const TopkParams &P, double a, double n, int lane) {
+    const int wl = P.lanes_log + 2;
+    auto join = [&](auto st) {
+        constexpr int ST = decltype(st)::value;
+        if ((1 << wl) <= ST) return;
+        auto other = [&](double v) {
+            const unsigned long long u = __builtin_bit_cast(unsigned long long, v);
+            return __builtin_bit_cast(
+                double, ((unsigned long long)xor_lane<ST>((uint32_t)(u >> 32), lane) << 32) |
+                            xor_lane<ST>((uint32_t)u, lane));
+        };
+        const double a2 = other(a), n2 = other(n);
+        n = fmax(fmin(a, a2), fmax(n, n2));
+        a = fmax(a, a2);
+    };
+    join(std::integral_constant<int, 1>{});
+    join(std::integral_constant<int, 2>{});
+    join(std::integral_constant<int, 4>{});
+    join(std::integral_constant<int, 8>{});
+    join(std::integral_constant<int, 16>{});
+    const double v = (P.flags & PP_GROUP_TOP2) && n > -INFINITY ? a + n : a;
+    const unsigned long long u = __builtin_bit_cast(unsigned long long, v);
+    int front = 0;
+#pragma unroll 1
+    for (int g = 0; g < P.n_groups; ++g) {
+        const unsigned long long ou =
+            ((unsigned long long)(uint32_t)__builtin_amdgcn_readlane((int)(u >> 32), g << wl)
+             << 32) | (uint32_t)__builtin_amdgcn_readlane((int)u, g << wl);
+        const double o = __builtin_bit_cast(double, ou);
+        front += o > v || (o == v && g < lane >> wl) ? 1 : 0;
+    }
+    return front;
+}
+
+// The groups of a row that stay, by scores in 64 bits: bit g << (lanes_log + 2)
+// for group g.  For a call with a bias, or worth two scores without one
+// (whose softmax scores need no sum for that).  zr, zb: the row and the bias.
+__device__ __forceinline__ unsigned long long exact_groups(const TopkParams &P, const float *zr,
+                                                           const float *zb, float zmax, int lane) {
+    const int wl = P.lanes_log + 2, grp = lane >> wl;
+    const bool sig = (P.flags & PP_SCORE_SIGMOID) != 0;
+    double a = -INFINITY, n = -INFINITY;
+    if (grp < P.n_groups) {
+#pragma unroll 1
+        for (int i = lane & ((1 << wl) - 1); i < P.Gs; i += 1 << wl) {
+            const float z = zr[grp * P.Gp + i];
+            const float b = P.sel_bias ? zb[grp * P.Gp + i] : 0.0f;
+            double v = sig ? sigmoid64(z) : exp_neg((double)z - (double)zmax);
+            v += (double)b;
+            if (z > -INFINITY && b > -INFINITY) {
+                n = fmax(n, fmin(a, v));
+                a = fmax(a, v);
+            }
+        }
+    }
+    return __ballot(groups_in_front(P, a, n, lane) < P.top_groups);
+}
+
 // Puts the n <= 64 listed experts in order of c (equal ones by index), of
 // which the first k are kept.
 __device__ __forceinline__ void sort_list(const double *c, short *list, int n, int k, int lane) {
@@ -556,9 +617,20 @@ __global__ __launch_bounds__(64 * kTopkWaves) void route_topk_k(TopkParams P) {
                 front += o > v || (o == v && before) ? 1 : 0;
             }
         });
-        if (SCORES)
-            unsure |= v > -INFINITY && front < P.top_groups && near >= P.top_groups;
         out = front >= P.top_groups;
+        if constexpr (SCORES) {
+            const unsigned long long open =
+                __ballot(v > -INFINITY && front < P.top_groups && near >= P.top_groups);
+            if (open != 0ull) {
+#pragma unroll 1
+                for (int r = 0; r < kRowsPerWave; ++r) {
+                    if (!((open >> (16 * r)) & 0xFFFFull)) continue;
+                    const unsigned long long stay = exact_groups(
+                        P, zs + r * P.Rp, zb, __shfl(zmax, 16 * r, 64), lane);
+                    if (rr == r) out = !((stay >> (grp << (P.lanes_log + 2))) & 1ull);
+                }
+            }
+        }
     }
     if (SCORES && !biased) {  // then experts are in the order of the logits
         err = 0.0f;
@@ -654,11 +726,10 @@ __global__ __launch_bounds__(64 * kTopkWaves) void route_topk_k(TopkParams P) {
     if (t < P.T) store_row<16>(P, zr, zmax, Sinv, pk + rr * kp, t, c16);
 }
 
-// One token a wavefront: the same choice, made in 64 bits at once, for few
-// tokens (a wavefront's work is spread over 64 lanes: 64 tokens of 256 experts
-// in 8 groups MEASURE_WIDE us) and for softmax scores plus a bias, which need
-// every score in 64 bits.  A group has 64 lanes over the next power of two of
-// n_groups; the passes' minimum is a scalar.
+// One token a wavefront: the same choice, made in 64 bits at once.  For softmax
+// scores plus a bias, which need every score in 64 bits, and for few tokens of
+// many experts (launch_topk).  A group has 64 lanes over the next power of two
+// of n_groups; the passes' minimum is a scalar.
 template <int NQ>
 __global__ __launch_bounds__(64 * kTopkWaves) void route_topk_wide_k(TopkParams P) {
     extern __shared__ __align__(16) float all_lds[];
@@ -753,35 +824,7 @@ __global__ __launch_bounds__(64 * kTopkWaves) void route_topk_wide_k(TopkParams 
             n = fmax(n, fmin(a, v));
             a = fmax(a, v);
         }
-        auto join = [&](auto st) {
-            constexpr int ST = decltype(st)::value;
-            if ((1 << wl) <= ST) return;
-            auto other = [&](double v) {
-                const unsigned long long u = __builtin_bit_cast(unsigned long long, v);
-                return __builtin_bit_cast(
-                    double, ((unsigned long long)xor_lane<ST>((uint32_t)(u >> 32), lane) << 32) |
-                                xor_lane<ST>((uint32_t)u, lane));
-            };
-            const double a2 = other(a), n2 = other(n);
-            n = fmax(fmin(a, a2), fmax(n, n2));
-            a = fmax(a, a2);
-        };
-        join(std::integral_constant<int, 1>{});
-        join(std::integral_constant<int, 2>{});
-        join(std::integral_constant<int, 4>{});
-        join(std::integral_constant<int, 8>{});
-        join(std::integral_constant<int, 16>{});
-        const double v = top2 && n > -INFINITY ? a + n : a;
-        const unsigned long long u = __builtin_bit_cast(unsigned long long, v);
-        int front = 0;
-#pragma unroll 1
-        for (int g = 0; g < P.n_groups; ++g) {
-            const unsigned long long ou =
-                ((unsigned long long)(uint32_t)__builtin_amdgcn_readlane((int)(u >> 32), g << wl)
-                 << 32) | (uint32_t)__builtin_amdgcn_readlane((int)u, g << wl);
-            const double o = __builtin_bit_cast(double, ou);
-            front += o > v || (o == v && g < grp) ? 1 : 0;
-        }
+        const int front = groups_in_front(P, a, n, lane);
 #pragma unroll
         for (int q = 0; q < NQ; ++q) c[q] = front < P.top_groups ? c[q] : -INFINITY;
     }
@@ -1068,7 +1111,11 @@ constexpr TopkWideBuild kTopkWideBuilds[] = {{1, route_topk_wide_k<1>},
                                              {2, route_topk_wide_k<2>},
                                              {4, route_topk_wide_k<4>},
                                              {7, route_topk_wide_k<7>}};
-// Up to so many tokens take a wavefront each.
+// Up to so many tokens take a wavefront each if 16 lanes would hold more than
+// 8 values each, which makes the passes long: 256 experts, k 8, 64 tokens 4.7
+// against 5.7 us with 16 lanes each, 1024 tokens 5.1 against 5.8, 4096 tokens
+// 6.9 against 6.0.  With fewer values the 16 lanes are no slower (112 experts,
+// 64 tokens: 4.5 against 4.2 us).
 constexpr int kWideTokens = 1024;
 
 hipError_t launch_topk(TopkParams P, hipStream_t s) {
@@ -1078,17 +1125,17 @@ hipError_t launch_topk(TopkParams P, hipStream_t s) {
     P.lanes = 1 << P.lanes_log;
     P.by_Gs = (uint32_t)((65536 + P.Gs - 1) / P.Gs);
     P.kp = P.k > kMaxList ? (P.k + 15) & ~15 : kMaxList;
-    if (P.T <= kWideTokens || (P.sel_bias && !(P.flags & PP_SCORE_SIGMOID))) {
-        const TopkWideBuild *B = kTopkWideBuilds;
-        while (B->values * 4 * P.lanes < P.Gs) ++B;  // at most 7
+    const TopkBuild *B = kTopkBuilds;
+    while (B->values * P.lanes < P.Gs) ++B;  // at most 28: nine groups of 28, a lane each
+    if ((P.T <= kWideTokens && B->values > 8) || (P.sel_bias && !(P.flags & PP_SCORE_SIGMOID))) {
+        const TopkWideBuild *W = kTopkWideBuilds;
+        while (W->values * 4 * P.lanes < P.Gs) ++W;  // at most 7
         P.Gp = P.Gs;
         P.wave_lds = 4 * kMaxExperts + P.kp / 2;
-        hipLaunchKernelGGL(B->kernel, dim3((P.T + kTopkWaves - 1) / kTopkWaves),
+        hipLaunchKernelGGL(W->kernel, dim3((P.T + kTopkWaves - 1) / kTopkWaves),
                            dim3(64 * kTopkWaves), sizeof(float) * kTopkWaves * P.wave_lds, s, P);
         return hipGetLastError();
     }
-    const TopkBuild *B = kTopkBuilds;
-    while (B->values * P.lanes < P.Gs) ++B;  // at most 28: nine groups of 28, a lane each
     // a group starts `lanes` banks after the one before, so that the 16 lanes
     // of a row read 16 different banks; one group: rows 16 banks apart
     P.Gp = (B->values * P.lanes + 31) / 32 * 32 + P.lanes;

@@ -64,6 +64,11 @@ def check(g, c):
     tiny = 1.2e-38 * abs(c["scale"])
     assert (np.abs(w - ref_w) <= weight_tolerance(g, idx) * np.abs(ref_w) + tiny).all()
     assert (w[idx < 0] == 0).all()
+    # the rows again and again in a long batch, which other kernels serve: the same bits
+    reps = 4100 // g.shape[0] + 1
+    ib, wb = route(np.tile(g, (reps, 1)), c)
+    np.testing.assert_array_equal(ib, np.tile(idx, (reps, 1)))
+    np.testing.assert_array_equal(wb.view(np.int32), np.tile(w.view(np.int32), (reps, 1)))
     return idx, w
 
 
@@ -91,12 +96,15 @@ def test_choice_and_weights(T, E, k, G, top, sigmoid):
 
 def test_tokens_do_not_touch_each_other():
     """A token alone, and among others at any place, gets the same bits."""
-    g = logits(513, 112, 4)
-    c = case(8, 4, 2, logits(1, 112, 5, 0.1)[0], 1.0, True, True, True)
-    idx, w = route(g, c)
-    for t in (0, 1, 63, 64, 300, 512):
-        i1, w1 = route(g[t:t + 1], c)
-        assert (i1[0] == idx[t]).all() and w1[0].tobytes() == w[t].tobytes()
+    for T, c in ((513, case(8, 4, 2, logits(1, 112, 5, 0.1)[0], 1.0, True, True, True)),
+                 (3001, case(8, 4, 2, logits(1, 112, 5, 0.1)[0], 1.0, True, False, True)),
+                 (3001, case(9, 7, 3, None, 1.0, False, False, True)),
+                 (3001, case(8, 1, 1, logits(1, 112, 5, 0.1)[0], 1.0, False, False, False))):
+        g = logits(T, 112, 4)
+        idx, w = route(g, c)
+        for t in (0, 1, 63, 64, 300, 512, T - 1):
+            i1, w1 = route(g[t:t + 1], c)
+            assert (i1[0] == idx[t]).all() and w1[0].tobytes() == w[t].tobytes()
 
 
 @pytest.mark.parametrize("sigmoid", [False, True])
@@ -185,10 +193,16 @@ def test_many_tokens_choice():
     rng = np.random.default_rng(12)
     g = (rng.standard_normal((T, E)) * 3 * np.exp(0.5 * rng.standard_normal((T, 1)))).astype(np.float32)
     bias = (rng.standard_normal(E) * 0.05).astype(np.float32)
-    idx, _ = route(g, case(k, 1, 1, bias, 1.0, True, True))
-    c = torch.sigmoid(torch.from_numpy(g).double()) + torch.from_numpy(bias).double()
-    ref = c.sort(dim=1, descending=True, stable=True).indices[:, :k].int().numpy()
-    np.testing.assert_array_equal(idx, ref)
+    s = torch.sigmoid(torch.from_numpy(g).double())
+    for G, top, b in ((1, 1, bias), (8, 4, bias), (8, 3, None), (16, 5, None)):
+        idx, _ = route(g, case(k, G, top, b, 1.0, True, True, True))
+        c = torch.from_numpy(g).double() if b is None else s + torch.from_numpy(b).double()
+        worth = (s if b is None else c).view(T, G, E // G).sort(dim=2, descending=True).values
+        groups = worth[:, :, :2].sum(2).sort(dim=1, descending=True, stable=True).indices[:, :top]
+        keep = torch.zeros((T, G), dtype=torch.bool).scatter_(1, groups, True)
+        c = c.masked_fill(~keep.repeat_interleave(E // G, 1), -float("inf"))
+        ref = c.sort(dim=1, descending=True, stable=True).indices[:, :k].int().numpy()
+        np.testing.assert_array_equal(idx, ref)
 
 
 # ------------------------------------------------------------------ gradient
