@@ -19,32 +19,43 @@ struct RoutedParams {
     float *gsig;         // [T][E], written for kept pairs only
 };
 
-// One token on one wavefront.  mark(e) records the pair and returns whether
-// this token had named e before.
+// The slots of n tokens from t0 on, one a thread at a time.  mark(t, e) records
+// that token t0 + t named e and returns whether it had named it before;
+// twice: LDS flags of the n tokens, cleared by the caller.
+// Bound by one round trip to memory (indices and weights are loaded together).
 template <typename Mark>
-__device__ __forceinline__ void scatter_token(const RoutedParams &P, int t, int lane, Mark mark) {
-    const int32_t *idx = P.idx + (size_t)t * P.k;
-    const float *w = P.w ? P.w + (size_t)t * P.k : nullptr;
-    float *gs = P.gsig + (size_t)t * P.E;
-    bool dup = false;
-    for (int j = lane; j < P.k; j += 64) {
-        const int e = idx[j];
-        if ((unsigned)e < (unsigned)P.E) dup |= mark(e);
+__device__ __forceinline__ void scatter_tokens(const RoutedParams &P, int t0, int n, int *twice,
+                                               Mark mark) {
+    const int32_t *idx = P.idx + (size_t)t0 * P.k;
+    const float *w = P.w ? P.w + (size_t)t0 * P.k : nullptr;
+    float *gs = P.gsig + (size_t)t0 * P.E;
+    const int slots = n * P.k, th = (int)blockDim.x;
+    auto store = [&](int s, int e, float v) {
+        const int t = s / P.k;
+        if ((unsigned)e < (unsigned)P.E && !twice[t]) gs[(size_t)t * P.E + e] = v;
+    };
+    const int s0 = (int)threadIdx.x;
+    const int e0 = s0 < slots ? idx[s0] : -1;
+    const float w0 = s0 < slots && w ? w[s0] : 1.0f;
+    if ((unsigned)e0 < (unsigned)P.E && mark(s0 / P.k, e0)) twice[s0 / P.k] = 1;
+    for (int s = s0 + th; s < slots; s += th) {
+        const int e = idx[s];
+        if ((unsigned)e < (unsigned)P.E && mark(s / P.k, e)) twice[s / P.k] = 1;
     }
-    if (__ballot(dup) == 0ull) {
-        for (int j = lane; j < P.k; j += 64) {
-            const int e = idx[j];
-            if ((unsigned)e < (unsigned)P.E) gs[e] = w ? w[j] : 1.0f;
-        }
-    } else if (lane == 0) {
-        // an expert twice: one lane adds the weights in slot order
+    __syncthreads();
+    if (s0 < slots) store(s0, e0, w0);
+    for (int s = s0 + th; s < slots; s += th) store(s, idx[s], w ? w[s] : 1.0f);
+    for (int t = s0; t < n; t += th) {
+        if (!twice[t]) continue;
+        // an expert twice: one thread adds the weights in slot order
         for (int j = 0; j < P.k; ++j) {
-            const int e = idx[j];
-            if ((unsigned)e < (unsigned)P.E) gs[e] = 0.0f;
+            const int e = idx[t * P.k + j];
+            if ((unsigned)e < (unsigned)P.E) gs[(size_t)t * P.E + e] = 0.0f;
         }
         for (int j = 0; j < P.k; ++j) {
-            const int e = idx[j];
-            if ((unsigned)e < (unsigned)P.E) gs[e] += w ? w[j] : 1.0f;
+            const int e = idx[t * P.k + j];
+            if ((unsigned)e < (unsigned)P.E)
+                gs[(size_t)t * P.E + e] += w ? w[t * P.k + j] : 1.0f;
         }
     }
 }
@@ -54,30 +65,32 @@ __device__ __forceinline__ void scatter_token(const RoutedParams &P, int t, int 
 __global__ __launch_bounds__(1024) void routed_decode_k(RoutedParams P,
                                                         unsigned long long *__restrict__ emask) {
     __shared__ unsigned long long em[kMaxExperts];
-    const int tid = threadIdx.x, lane = tid & 63;
+    __shared__ int twice[kDecodeTile];
+    const int tid = threadIdx.x;
     if (tid < kMaxExperts) em[tid] = 0ull;
+    if (tid < kDecodeTile) twice[tid] = 0;
     __syncthreads();
-    for (int t = tid >> 6; t < P.T; t += 16)
-        scatter_token(P, t, lane, [&](int e) {
-            return ((atomicOr(&em[e], 1ull << t) >> t) & 1ull) != 0ull;
-        });
-    __syncthreads();
+    scatter_tokens(P, 0, P.T, twice, [&](int t, int e) {
+        return ((atomicOr(&em[e], 1ull << t) >> t) & 1ull) != 0ull;
+    });
     if (tid < P.E) emask[tid] = em[tid];
 }
 
+constexpr int kRoutedTokens = 32;  // of a prefill workgroup: 8 slots a token keep 256 threads busy
 __global__ __launch_bounds__(256) void routed_prefill_k(RoutedParams P,
                                                         uint32_t *__restrict__ selmask) {
-    __shared__ uint32_t sm[4][8];
-    const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6;
-    const int t = blockIdx.x * 4 + wv;
-    if (lane < 8) sm[wv][lane] = 0u;
+    __shared__ uint32_t sm[kRoutedTokens][8];
+    __shared__ int twice[kRoutedTokens];
+    const int tid = threadIdx.x, t0 = blockIdx.x * kRoutedTokens;
+    const int n = min(kRoutedTokens, P.T - t0);
+    static_assert(kRoutedTokens * 8 == 256, "a mask word a thread");
+    sm[tid >> 3][tid & 7] = 0u;
+    if (tid < kRoutedTokens) twice[tid] = 0;
     __syncthreads();
-    if (t < P.T)
-        scatter_token(P, t, lane, [&](int e) {
-            return ((atomicOr(&sm[wv][e >> 5], 1u << (e & 31)) >> (e & 31)) & 1u) != 0u;
-        });
-    __syncthreads();
-    if (t < P.T && lane < 8) selmask[(size_t)t * 8 + lane] = sm[wv][lane];
+    scatter_tokens(P, t0, n, twice, [&](int t, int e) {
+        return ((atomicOr(&sm[t][e >> 5], 1u << (e & 31)) >> (e & 31)) & 1u) != 0u;
+    });
+    if ((tid >> 3) < n) selmask[(size_t)t0 * 8 + tid] = sm[tid >> 3][tid & 7];
 }
 
 pp_status run_routed(pp_layer *L, const uint16_t *x, int32_t T, int32_t k, const int32_t *idx,
@@ -93,7 +106,8 @@ pp_status run_routed(pp_layer *L, const uint16_t *x, int32_t T, int32_t k, const
                                 L->gsig};
         prof_mark(L, PP_KERNEL_ROUTE, s, true);
         if (prefill)
-            hipLaunchKernelGGL(routed_prefill_k, dim3((n + 3) / 4), dim3(256), 0, s, P, L->selmask);
+            hipLaunchKernelGGL(routed_prefill_k, dim3((n + kRoutedTokens - 1) / kRoutedTokens),
+                               dim3(256), 0, s, P, L->selmask);
         else
             hipLaunchKernelGGL(routed_decode_k, dim3(1), dim3(1024), 0, s, P, L->emask);
         prof_mark(L, PP_KERNEL_ROUTE, s, false);
