@@ -278,6 +278,41 @@ def test_replayed_graph_gives_the_eager_bits():
             assert torch.equal(a, e)
 
 
+def test_offsets_past_32_bits():
+    """More than 2^31 values: the last rows as in a call of their own, forward and back."""
+    import torch
+    T, d, n = 525000, 4096, 3
+    x = torch.randn((T, d), device="cuda")
+    u = torch.empty((T, d), dtype=torch.bfloat16, device="cuda")
+    w, b, st = torch.randn(d, device="cuda"), torch.randn(d, device="cuda"), torch.empty((T, 2), device="cuda")
+    pp.prunepath_residual_layernorm(x, None, None, T, d, EPS, w, b, u, st)
+    u2, st2 = torch.empty_like(u[:n]), torch.empty_like(st[:n])
+    pp.prunepath_residual_layernorm(x[-n:], None, None, n, d, EPS, w, b, u2, st2)
+    assert torch.equal(u[-n:], u2) and torch.equal(st[-n:], st2)
+    dx, dw, db = torch.empty_like(x), torch.empty(d, device="cuda"), torch.empty(d, device="cuda")
+    ws = torch.empty(pp.prunepath_residual_layernorm_grad_workspace(T, d), dtype=torch.uint8,
+                     device="cuda")
+    pp.prunepath_residual_layernorm_grad(x, u, None, T, d, w, st, dx, dw, db, ws)
+    dx2 = torch.empty_like(x[:n])
+    pp.prunepath_residual_layernorm_grad(x[-n:], u2, None, n, d, w, st2, dx2)
+    assert torch.equal(dx[-n:], dx2)
+    # db: 525000 values of about |b| <= 5, fp32 chains of T / 512 additions and 512 partial sums
+    ref = torch.zeros(d, dtype=torch.float64, device="cuda")
+    size = torch.zeros(d, dtype=torch.float64, device="cuda")
+    for i in range(0, T, 75000):
+        ref += u[i:i + 75000].double().sum(0)
+        size += u[i:i + 75000].double().abs().sum(0)
+    assert ((db.double() - ref).abs() <= (T / 512 + 16) * HALF * size).all()
+
+
+@pytest.mark.parametrize("d", [3, 32])
+def test_many_short_rows(d):
+    T = 150001
+    x, y, w, b = data(T, d, d)
+    check_forward(x, y, w, b, True)
+    check_backward(T, d, d, False)
+
+
 def test_binding_refuses_short_arrays():
     import torch
     x, u = torch.zeros((4, 8), device="cuda"), torch.zeros((4, 8), dtype=torch.bfloat16, device="cuda")

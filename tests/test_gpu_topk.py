@@ -205,6 +205,47 @@ def test_many_tokens_choice():
         np.testing.assert_array_equal(idx, ref)
 
 
+@pytest.mark.parametrize("E,k,G,top", [(256, 20, 1, 1), (256, 80, 1, 1), (250, 100, 5, 3),
+                                       (256, 64, 8, 4), (64, 63, 1, 1)])
+@pytest.mark.parametrize("sigmoid", [False, True])
+def test_many_equal_logits(E, k, G, top, sigmoid):
+    """Logits and biases of a few values each: ties in and around the cut, of experts and groups."""
+    rng = np.random.default_rng(E + k)
+    g = (np.round(rng.standard_normal((5, E)) * 4) / 4).astype(np.float32)
+    g[3] = 0.5
+    g[4, ::3] = -np.inf
+    for bias in (None, np.zeros(E, np.float32), (rng.integers(0, 3, E) / 8).astype(np.float32)):
+        for top2 in (False, True):
+            check(g, case(k, G, top, bias, 1.0, sigmoid, True, top2))
+
+
+def test_signalling_nans_take_no_part():
+    g = logits(3, 40, 23)
+    bits = g.view(np.uint32)
+    bits[0, 3], bits[0, 39], bits[1, :] = 0x7F800001, 0xFF812345, 0x7FA00000
+    for c in (case(5), case(5, sigmoid=True, renorm=True), case(3, 4, 2, sigmoid=True, top2=True),
+              case(5, sel_bias=np.full(40, 0.25, np.float32), sigmoid=True)):
+        idx, _ = check(g, c)
+        assert 3 not in idx[0] and 39 not in idx[0] and (idx[1] == -1).all()
+
+
+def test_offsets_past_32_bits():
+    """2^22 rows of 256 logits (4 GiB): the last rows as in a call of their own, forward and back."""
+    import torch
+    T, E, k, n = 1 << 22, 256, 2, 5
+    g = torch.randn((T, E), device="cuda")
+    idx, w = torch.zeros((T, k), dtype=torch.int32, device="cuda"), torch.zeros((T, k), device="cuda")
+    dw, dg = torch.randn((T, k), device="cuda"), torch.empty((T, E), device="cuda")
+    fl = pp.PP_SCORE_SIGMOID | pp.PP_TOPK_RENORM
+    pp.prunepath_route_topk_logits(g, T, E, k, 1, 1, None, 1.0, fl, idx, w)
+    pp.prunepath_route_topk_grad(g, T, E, k, idx, dw, 1.0, fl, dg)
+    tail = [a[-n:].clone() for a in (g, idx, w, dw, dg)]
+    i2, w2, d2 = torch.zeros_like(tail[1]), torch.zeros_like(tail[2]), torch.zeros_like(tail[4])
+    pp.prunepath_route_topk_logits(tail[0], n, E, k, 1, 1, None, 1.0, fl, i2, w2)
+    pp.prunepath_route_topk_grad(tail[0], n, E, k, i2, tail[3], 1.0, fl, d2)
+    assert torch.equal(i2, tail[1]) and torch.equal(w2, tail[2]) and torch.equal(d2, tail[4])
+
+
 # ------------------------------------------------------------------ gradient
 
 def grad(g, idx, dw, c, add=None):
@@ -387,6 +428,37 @@ def test_handle_route(T):
         np.testing.assert_array_equal(idx.cpu().numpy(), ri)
         np.testing.assert_array_equal(w.cpu().numpy(), rw)
     finally:
+        pp.prunepath_destroy(h)
+
+
+@pytest.mark.parametrize("T", [1, 3, 70])
+@pytest.mark.parametrize("E,G,top", [(160, 1, 1), (160, 8, 3), (24, 1, 1)])
+@pytest.mark.parametrize("sigmoid", [False, True])
+def test_handle_route_rules(T, E, G, top, sigmoid):
+    """Biases, groups and many experts on a handle's router: the choice and the weights of the call
+    on the logits that it reports, bit for bit (d 1088: three K-slices, the last of one K-step)."""
+    import torch
+    d, k = 1088, 6
+    torch.manual_seed(T + E)
+    bf = lambda *s: torch.randn(s, device="cuda").mul_(0.05).bfloat16()  # noqa: E731
+    x = torch.randn((T, d), device="cuda").bfloat16()
+    bias = torch.randn(E, device="cuda") * 0.1
+    fl = (pp.PP_SCORE_SIGMOID if sigmoid else 0) | pp.PP_GROUP_TOP2
+    h = pp.prunepath_create(d, 128 * E, E, 128, bf(E, d), bf(128 * E, d), bf(128 * E, d),
+                            bf(d, 128 * E))
+    try:
+        for b in (None, bias):
+            g = torch.full((T, E), float("nan"), device="cuda")
+            idx, w = torch.zeros((T, k), dtype=torch.int32, device="cuda"), torch.zeros((T, k), device="cuda")
+            i2, w2 = torch.ones_like(idx), torch.ones_like(w)
+            pp.prunepath_route_topk(h, x, T, None, k, G, top, b, 1.5, fl, idx, w, g)
+            pp.prunepath_route_topk_logits(g, T, E, k, G, top, b, 1.5, fl, i2, w2)
+            assert torch.equal(idx, i2) and torch.equal(w, w2)
+            ri, _ = op.route_topk(g.cpu().numpy(), k, G, top, None if b is None else b.cpu().numpy(),
+                                  1.5, sigmoid, False, True)
+            np.testing.assert_array_equal(idx.cpu().numpy(), ri)
+    finally:
+        torch.cuda.synchronize()
         pp.prunepath_destroy(h)
 
 
