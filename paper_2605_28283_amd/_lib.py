@@ -174,7 +174,7 @@ def _arg(a, kind, n, name, dev):
     if a is None or isinstance(a, int):
         return a
     if (a.get_device() == dev and a.is_contiguous() and a.numel() >= n
-            and (kind is None or a.dtype in _kinds()[kind])):
+            and (kind is None or a.dtype in (_KINDS or _kinds())[kind])):
         return a.data_ptr()
     _ptr(a, kind)  # raises for anything but the device and the size
     if a.get_device() != dev:
@@ -182,19 +182,35 @@ def _arg(a, kind, n, name, dev):
     raise ValueError("%s: %d elements, the call needs %d" % (name, a.numel(), n))
 
 
-def _device():
-    """The current device's index."""
-    import torch
-    return torch.cuda.current_device()
+_current = None  # (current device's index, its current stream's handle by index)
+
+
+def _current_calls():
+    """torch's calls for the current device and stream: the ones that return
+    plain numbers, where this torch has them (0.1 us; the stream's object
+    takes 3)."""
+    global _current
+    if _current is None:
+        import torch
+        device = getattr(torch._C, "_cuda_getDevice", None)
+        stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+        torch.cuda.current_device()  # initialises the device
+        _current = (device or torch.cuda.current_device,
+                    stream or (lambda i: torch.cuda.current_stream(i).cuda_stream))
+    return _current
+
+
+def _place(stream):
+    """(current device's index, handle of `stream` or of the current one)."""
+    device, raw = _current or _current_calls()
+    i = device()
+    return i, raw(i) if stream is None else _stream(stream)
 
 
 def _stream(stream):
     if stream is None:
-        import torch
-        raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)  # 0.1 us; the object takes 3
-        if raw is not None:
-            return raw(torch.cuda.current_device())
-        return torch.cuda.current_stream().cuda_stream
+        device, raw = _current or _current_calls()
+        return raw(device())
     if isinstance(stream, int):
         return stream
     return stream.cuda_stream
@@ -265,43 +281,43 @@ def prunepath_residual_rmsnorm(x, y, x_out, T, d, eps, u=None, stream=None):
 def prunepath_route_topk(handle, x, T, inv_temp, k, n_groups, top_groups, sel_bias, scale, flags,
                          expert_idx, gate_w, logits=None, stream=None):
     """k experts per token by the handle's router (include/prunepath.h has the rule)."""
-    v = _device()
+    v, stream = _place(stream)
     st = load().prunepath_route_topk(
         handle, _arg(x, "bf16", 0, "x", v), T, _arg(inv_temp, "f32", T, "inv_temp", v), k,
         n_groups, top_groups, _arg(sel_bias, "f32", 0, "sel_bias", v), scale, flags,
         _arg(expert_idx, "i32", T * k, "expert_idx", v), _arg(gate_w, "f32", T * k, "gate_w", v),
-        _arg(logits, "f32", 0, "logits", v), _stream(stream))
+        _arg(logits, "f32", 0, "logits", v), stream)
     _check(st, "prunepath_route_topk")
 
 
 def prunepath_route_topk_logits(g, T, E, k, n_groups, top_groups, sel_bias, scale, flags,
                                 expert_idx, gate_w, stream=None):
     """k experts per row of the logits g [T, E]."""
-    v = _device()
+    v, stream = _place(stream)
     st = load().prunepath_route_topk_logits(
         _arg(g, "f32", T * E, "g", v), T, E, k, n_groups, top_groups,
         _arg(sel_bias, "f32", E, "sel_bias", v), scale, flags,
         _arg(expert_idx, "i32", T * k, "expert_idx", v), _arg(gate_w, "f32", T * k, "gate_w", v),
-        _stream(stream))
+        stream)
     _check(st, "prunepath_route_topk_logits")
 
 
 def prunepath_route_topk_grad(g, T, E, k, expert_idx, dgate_w, scale, flags, dg, stream=None):
     """dg = dL/dg of the rows' weights (added to dg with PP_GRAD_ADD)."""
-    v = _device()
+    v, stream = _place(stream)
     st = load().prunepath_route_topk_grad(
         _arg(g, "f32", T * E, "g", v), T, E, k, _arg(expert_idx, "i32", T * k, "expert_idx", v),
         _arg(dgate_w, "f32", T * k, "dgate_w", v), scale, flags, _arg(dg, "f32", T * E, "dg", v),
-        _stream(stream))
+        stream)
     _check(st, "prunepath_route_topk_grad")
 
 
 def _ffn_routed(name, handle, x, T, k, expert_idx, gate_w, y, stream):
-    v = _device()
+    v, stream = _place(stream)
     st = getattr(load(), name)(handle, _arg(x, "bf16", 0, "x", v), T, k,
                                _arg(expert_idx, "i32", T * k, "expert_idx", v),
                                _arg(gate_w, "f32", T * k, "gate_w", v), _arg(y, "f32", 0, "y", v),
-                               _stream(stream))
+                               stream)
     _check(st, name)
 
 
@@ -318,12 +334,12 @@ def prunepath_ffn_prefill_routed(handle, x, T, k, expert_idx, gate_w, y, stream=
 def prunepath_residual_layernorm(x, y, x_out, T, d, eps, w, b, u, stats=None, flags=0,
                                  stream=None):
     """x_out = x + y, u = its layer norm (y, x_out, w, b, stats may be None)."""
-    v, n = _device(), T * d
+    (v, stream), n = _place(stream), T * d
     st = load().prunepath_residual_layernorm(
         _arg(x, "f32", n, "x", v), _arg(y, "f32", n, "y", v), _arg(x_out, "f32", n, "x_out", v),
         T, d, eps, _arg(w, "f32", d, "w", v), _arg(b, "f32", d, "b", v),
         _arg(u, "f32" if flags & PP_NORM_F32 else "bf16", n, "u", v),
-        _arg(stats, "f32", 2 * T, "stats", v), flags, _stream(stream))
+        _arg(stats, "f32", 2 * T, "stats", v), flags, stream)
     _check(st, "prunepath_residual_layernorm")
 
 
@@ -335,7 +351,7 @@ def prunepath_residual_layernorm_grad_workspace(T, d):
 def prunepath_residual_layernorm_grad(x_out, du, dres, T, d, w, stats, dx, dw=None, db=None,
                                       workspace=None, flags=0, stream=None):
     """dx, and dw and db unless None (then without a workspace if both are)."""
-    v, n, lib = _device(), T * d, load()
+    (v, stream), n, lib = _place(stream), T * d, load()
     ws = _arg(workspace, None, 0, "workspace", v)
     if (dw is not None or db is not None) and ws is not workspace:
         need = lib.prunepath_residual_layernorm_grad_workspace(T, d)
@@ -346,7 +362,7 @@ def prunepath_residual_layernorm_grad(x_out, du, dres, T, d, w, stats, dx, dw=No
         _arg(du, "f32" if flags & PP_NORM_F32 else "bf16", n, "du", v),
         _arg(dres, "f32", n, "dres", v), T, d, _arg(w, "f32", d, "w", v),
         _arg(stats, "f32", 2 * T, "stats", v), _arg(dx, "f32", n, "dx", v),
-        _arg(dw, "f32", d, "dw", v), _arg(db, "f32", d, "db", v), ws, flags, _stream(stream))
+        _arg(dw, "f32", d, "dw", v), _arg(db, "f32", d, "db", v), ws, flags, stream)
     _check(st, "prunepath_residual_layernorm_grad")
 
 
