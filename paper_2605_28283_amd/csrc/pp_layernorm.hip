@@ -5,7 +5,10 @@
 //   dw = sum_t du hat,  db = sum_t du
 // Not part of the paper's method: the norm of the GELU-MLP blocks whose FFN
 // prunepath_create_mlp makes.  Bound by memory: each input is read once and
-// each output written once.
+// each output written once.  16384 x 4096 with bf16 u and du: 165 us forward
+// (5.7 TB/s of 0.94 GB), 178 us back (5.3 TB/s), where a 4 GiB copy moves 4.8
+// TB/s; at d 4095, column by column, 178 and 178 us; rows read again for every
+// sum took 910 us for both.
 //
 // A row of up to 8192 values stays in registers between its sums and its
 // outputs: one wavefront for up to 1024 (four rows a workgroup, no barrier),

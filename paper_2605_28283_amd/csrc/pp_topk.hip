@@ -9,18 +9,23 @@
 //   Chosen: the k largest c of the groups that stay, equal ones by ascending
 //   index.  w_j = scale s_j, or scale s_j / (sum of the chosen s).
 //
-// A token takes the 16 lanes of one DPP row, four tokens a wavefront.  The rows of logits (and the bias) are read in whole
-// cache lines into LDS; a lane then holds values of one group only (16 lanes
-// over the next power of two of n_groups), so a group's worth is a reduction
-// in registers and over few lanes.
-// The k passes run on 32-bit keys: the distance from the row's largest c,
-// rounded to a float, its low byte replaced by the expert, so that one
-// unsigned minimum gives value and index.  Scores are formed in 32 bits for
-// that; a choice that they leave open is made in 64 bits: up to 16 candidates,
-// one a lane, are put in order by their exact c; a row in which that many do
-// not hold everything next to the cut, or two groups are too near, is chosen
-// again from every c in 64 bits by the whole wavefront (choose_row).  So c is
-// compared in 64 bits wherever it matters, and few tokens pay for it.
+// A token takes the 16 lanes of one DPP row, four tokens a wavefront.  The
+// rows of logits (and the bias) are read in whole cache lines into LDS; a lane
+// then holds values of one group only (16 lanes over the next power of two of
+// n_groups), so a group's worth is a reduction in registers and over few lanes.
+// The k passes run on 32-bit keys: half the distance from the row's largest c,
+// its low byte replaced by the expert, so that one unsigned minimum gives value
+// and index.  Scores are formed in 32 bits for that, within a stated error;
+// what they leave open is decided in 64 bits by the whole wavefront: groups
+// too near each other (exact_groups), neighbours of the list too near each
+// other or to what was left out (the list, with all that may belong in it, is
+// sorted by exact c: sort_list), and rows where that is more than 64 entries
+// (choose_row).  So c is compared in 64 bits wherever it matters, and few
+// tokens pay for it.
+// Bound by vector instructions: 16384 tokens of 256 experts, 8 groups, k 8,
+// sigmoid plus a bias take 13.2 us (11.0 among captured calls) for 17.8 MB,
+// 1057 vector instructions a wavefront, of which the nine passes are a third;
+// every score in 64 bits took 28.8 us, an argmax over 64-bit values 50.7.
 // Weights are formed in fp32; renormalised ones from scores relative to the
 // largest chosen one, so a row of scores that all underflow still has them.
 // Deterministic: no floating-point atomics; a token's result does not depend
@@ -194,6 +199,11 @@ __device__ __forceinline__ float exp_fast(float x) {
 // with log2 e, the exponential), of which s^2 counts, at most 2.9e-7 for
 // either sign of z; 1 + e and its reciprocal add (2^-24 + 2^-23) s.
 constexpr float kScoreErr = 6e-7f;
+// Softmax scores p = e / S: e^-x is off by e (x 2^-22.5 + 2^-22) < 3.1e-7 (also
+// x = zmax - z was rounded); S, at least 1, by the mean of that over p, in
+// which x averages to at most log 256 (an entropy), and by 20 roundings:
+// 2.5e-6 relative.
+constexpr float kSoftmaxErr = 3.2e-6f;
 __device__ __forceinline__ float sigmoid_fast(float z) {
     return __builtin_amdgcn_rcpf(1.0f + exp_fast(-z));
 }
@@ -293,11 +303,26 @@ __device__ __forceinline__ int groups_in_front(const TopkParams &P, double a, do
     return front;
 }
 
+// 1 / (sum of e^(z - zmax)) of a row in 64 bits, by the whole wavefront.
+__device__ __forceinline__ double exact_softmax_scale(const TopkParams &P, const float *zr,
+                                                      float zmax, int lane) {
+    double S = 0.0;
+#pragma unroll 1
+    for (int e = lane; e < P.E; e += 64) {
+        const float z = zr[topk_place(P, e)];
+        if (z > -INFINITY) S += exp_neg((double)z - (double)zmax);
+    }
+    S = wave_reduce(S, lane, [](double a, double b) { return a + b; });
+    return S > 0.0 ? rcp64(S) : 0.0;
+}
+
 // The groups of a row that stay, by scores in 64 bits: bit g << (lanes_log + 2)
 // for group g.  For a call with a bias, or worth two scores without one
-// (whose softmax scores need no sum for that).  zr, zb: the row and the bias.
+// (whose softmax scores need no sum for that: scale 1).  zr, zb: the row and
+// the bias.
 __device__ __forceinline__ unsigned long long exact_groups(const TopkParams &P, const float *zr,
-                                                           const float *zb, float zmax, int lane) {
+                                                           const float *zb, float zmax,
+                                                           double scale, int lane) {
     const int wl = P.lanes_log + 2, grp = lane >> wl;
     const bool sig = (P.flags & PP_SCORE_SIGMOID) != 0;
     double a = -INFINITY, n = -INFINITY;
@@ -306,7 +331,7 @@ __device__ __forceinline__ unsigned long long exact_groups(const TopkParams &P, 
         for (int i = lane & ((1 << wl) - 1); i < P.Gs; i += 1 << wl) {
             const float z = zr[grp * P.Gp + i];
             const float b = P.sel_bias ? zb[grp * P.Gp + i] : 0.0f;
-            double v = sig ? sigmoid64(z) : exp_neg((double)z - (double)zmax);
+            double v = sig ? sigmoid64(z) : exp_neg((double)z - (double)zmax) * scale;
             v += (double)b;
             if (z > -INFINITY && b > -INFINITY) {
                 n = fmax(n, fmin(a, v));
@@ -338,8 +363,8 @@ __device__ __forceinline__ void sort_list(const double *c, short *list, int n, i
 // One row's choice, all of it in 64 bits, by the whole wavefront: lane l has
 // experts l, l + 64, ...  zr, zb: the row and the bias in LDS; zmax: the row's
 // largest logit; worth: 256 doubles of LDS; out: [k].
-__device__ __forceinline__ void choose_row(const TopkParams &P, const float *zr, const float *zb, float zmax,
-                           double *worth, short *out, int lane) {
+__device__ __forceinline__ void choose_row(const TopkParams &P, const float *zr, const float *zb,
+                                           float zmax, double *worth, short *out, int lane) {
     constexpr int NE = kMaxExperts / 64;
     const bool sig = (P.flags & PP_SCORE_SIGMOID) != 0;
     const bool top2 = (P.flags & PP_GROUP_TOP2) != 0;
@@ -429,7 +454,6 @@ __device__ __forceinline__ void store_row(const TopkParams &P, const float *zr, 
     const int k = P.k;
     float m = sig ? 0.0f : zmax, scale = sig ? P.scale : P.scale * Sinv;
     if (P.flags & PP_TOPK_RENORM) {
-        // sums over each 16 lanes, then over the rows of 16
         m = -INFINITY;
         for (int j = l; j < k; j += W) {
             const int e = list[j];
@@ -550,7 +574,7 @@ __global__ __launch_bounds__(64 * kTopkWaves) void route_topk_k(TopkParams P) {
 #pragma unroll
         for (int q = 1; q < NQ; ++q) zmax = num.max(zmax, c[q]);
         zmax = row_max(zmax);
-        if (!renorm) {
+        if (!renorm || biased) {
             float S = 0.0f;
 #pragma unroll
             for (int q = 0; q < NQ; ++q) S += exp_fast(c[q] - zmax);
@@ -566,7 +590,7 @@ __global__ __launch_bounds__(64 * kTopkWaves) void route_topk_k(TopkParams P) {
             for (int st = 1; st < 64; st <<= 1)
                 big = fmaxf(big, __uint_as_float(xor_lane_rt(__float_as_uint(big), st, lane)));
         }
-        err = kScoreErr + (1.0f + big) * 2.4e-7f;
+        err = (biased && !sig ? kSoftmaxErr : kScoreErr) + (1.0f + big) * 2.4e-7f;
         // (an expert that takes no part has a score of 0 here)
         float s[NQ];
         if (sig) {
@@ -575,6 +599,10 @@ __global__ __launch_bounds__(64 * kTopkWaves) void route_topk_k(TopkParams P) {
         } else {
 #pragma unroll
             for (int q = 0; q < NQ; ++q) s[q] = exp_fast(c[q] - zmax);
+            if (biased) {
+#pragma unroll
+                for (int q = 0; q < NQ; ++q) s[q] *= Sinv;
+            }
         }
         if (biased) {
             const float *const mb = zb + grp * P.Gp + sub;
@@ -625,8 +653,11 @@ __global__ __launch_bounds__(64 * kTopkWaves) void route_topk_k(TopkParams P) {
 #pragma unroll 1
                 for (int r = 0; r < kRowsPerWave; ++r) {
                     if (!((open >> (16 * r)) & 0xFFFFull)) continue;
-                    const unsigned long long stay = exact_groups(
-                        P, zs + r * P.Rp, zb, __shfl(zmax, 16 * r, 64), lane);
+                    const float top = __shfl(zmax, 16 * r, 64);
+                    const double scale =
+                        biased && !sig ? exact_softmax_scale(P, zs + r * P.Rp, top, lane) : 1.0;
+                    const unsigned long long stay =
+                        exact_groups(P, zs + r * P.Rp, zb, top, scale, lane);
                     if (rr == r) out = !((stay >> (grp << (P.lanes_log + 2))) & 1ull);
                 }
             }
@@ -706,10 +737,17 @@ __global__ __launch_bounds__(64 * kTopkWaves) void route_topk_k(TopkParams P) {
         for (int r = 0; r < kRowsPerWave; ++r) {
             if (!((sort >> (16 * r)) & 1ull)) continue;
             const int n = __builtin_amdgcn_readlane(len, 16 * r);
+            const float top = __shfl(zmax, 16 * r, 64);
+            double scale = 1.0;
+            if (biased && !sig) scale = exact_softmax_scale(P, zs + r * P.Rp, top, lane);
             if (lane < n) {
                 const int e = pk[r * kp + lane], at = topk_place(P, e);
                 const float x = zs[r * P.Rp + at];
-                worth[e] = biased ? sigmoid64(x) + (double)zb[at] : (double)x;
+                double v = (double)x;
+                if (biased)
+                    v = (sig ? sigmoid64(x) : exp_neg((double)x - (double)top) * scale) +
+                        (double)zb[at];
+                worth[e] = v;
             }
             sort_list(worth, pk + r * kp, n, k, lane);
         }
@@ -726,9 +764,8 @@ __global__ __launch_bounds__(64 * kTopkWaves) void route_topk_k(TopkParams P) {
     if (t < P.T) store_row<16>(P, zr, zmax, Sinv, pk + rr * kp, t, c16);
 }
 
-// One token a wavefront: the same choice, made in 64 bits at once.  For softmax
-// scores plus a bias, which need every score in 64 bits, and for few tokens of
-// many experts (launch_topk).  A group has 64 lanes over the next power of two
+// One token a wavefront: the same choice, made in 64 bits at once, for few
+// tokens of many experts (launch_topk).  A group has 64 lanes over the next power of two
 // of n_groups; the passes' minimum is a scalar.
 template <int NQ>
 __global__ __launch_bounds__(64 * kTopkWaves) void route_topk_wide_k(TopkParams P) {
@@ -919,7 +956,8 @@ struct TopkGradParams {
 //   sigmoid                 dg_e = scale s_e (1 - s_e) a_e
 //   renormalised softmax    dg_e = scale q_e (a_e - D)
 //   renormalised sigmoid    dg_e = scale q_e (1 - s_e) (a_e - D)
-// Bound by memory (dg is written whole).  A token takes 16 lanes: lane c has
+// Bound by memory (dg is written whole): 16384 x 112, k 16, plain softmax
+// 5.8 us for 22 MB; a wavefront a token with the slots in turn took 57.  A token takes 16 lanes: lane c has
 // slots c, c + 16, ... and columns c, c + 16, ... (NQ of them); the slots'
 // values meet the columns in LDS.  ROW: plain softmax, whose gradient reaches
 // every expert and needs the whole row; else only the slots' logits are read.
@@ -1107,9 +1145,7 @@ struct TopkWideBuild {
     int values;
     void (*kernel)(TopkParams);
 };
-constexpr TopkWideBuild kTopkWideBuilds[] = {{1, route_topk_wide_k<1>},
-                                             {2, route_topk_wide_k<2>},
-                                             {4, route_topk_wide_k<4>},
+constexpr TopkWideBuild kTopkWideBuilds[] = {{4, route_topk_wide_k<4>},
                                              {7, route_topk_wide_k<7>}};
 // Up to so many tokens take a wavefront each if 16 lanes would hold more than
 // 8 values each, which makes the passes long: 256 experts, k 8, 64 tokens 4.7
@@ -1127,7 +1163,7 @@ hipError_t launch_topk(TopkParams P, hipStream_t s) {
     P.kp = P.k > kMaxList ? (P.k + 15) & ~15 : kMaxList;
     const TopkBuild *B = kTopkBuilds;
     while (B->values * P.lanes < P.Gs) ++B;  // at most 28: nine groups of 28, a lane each
-    if ((P.T <= kWideTokens && B->values > 8) || (P.sel_bias && !(P.flags & PP_SCORE_SIGMOID))) {
+    if (P.T <= kWideTokens && B->values > 8) {
         const TopkWideBuild *W = kTopkWideBuilds;
         while (W->values * 4 * P.lanes < P.Gs) ++W;  // at most 7
         P.Gp = P.Gs;
