@@ -5,10 +5,10 @@
 //   dw = sum_t du hat,  db = sum_t du
 // Not part of the paper's method: the norm of the GELU-MLP blocks whose FFN
 // prunepath_create_mlp makes.  Bound by memory: each input is read once and
-// each output written once.  16384 x 4096 with bf16 u and du: 165 us forward
-// (5.7 TB/s of 0.94 GB), 178 us back (5.3 TB/s), where a 4 GiB copy moves 4.8
-// TB/s; at d 4095, column by column, 178 and 178 us; rows read again for every
-// sum took 910 us for both.
+// each output written once.  16384 x 4096 with bf16 u and du: 160 us forward
+// (5.9 TB/s of 0.94 GB), 157 us back (6.0 TB/s), where a 4 GiB copy moves 4.8
+// TB/s; at d 4095, column by column, 178 and 172 us.  (Rows read again for
+// every sum took 910 us for both.)
 //
 // A row of up to 8192 values stays in registers between its sums and its
 // outputs: one wavefront for up to 1024 (four rows a workgroup, no barrier),
@@ -56,55 +56,70 @@ __device__ __forceinline__ void row_totals(float (&v)[n], float *slot) {
     }
 }
 
-// V consecutive values of a row.
+// V consecutive values of a row.  NT: a nontemporal access, for arrays too
+// long to be in a cache when they are met again (ln_streams).
 template <int V>
 struct Cols {
     float v[V];
 };
-template <int V>
+typedef uint32_t u32x2_t __attribute__((ext_vector_type(2)));
+template <typename T, bool NT>
+__device__ __forceinline__ T load_as(const void *p) {
+    const T *q = static_cast<const T *>(p);
+    return NT ? __builtin_nontemporal_load(q) : *q;
+}
+template <typename T, bool NT>
+__device__ __forceinline__ void store_as(void *p, T v) {
+    T *q = static_cast<T *>(p);
+    if constexpr (NT)
+        __builtin_nontemporal_store(v, q);
+    else
+        *q = v;
+}
+template <int V, bool NT = false>
 __device__ __forceinline__ Cols<V> load_f32(const float *p) {
     Cols<V> c;
     if constexpr (V == 4) {
-        const float4 f = *reinterpret_cast<const float4 *>(p);
+        const f32x4 f = load_as<f32x4, NT>(p);
         c.v[0] = f.x, c.v[1] = f.y, c.v[2] = f.z, c.v[3] = f.w;
     } else {
-        c.v[0] = *p;
+        c.v[0] = load_as<float, NT>(p);
     }
     return c;
 }
-template <int V>
+template <int V, bool NT = false>
 __device__ __forceinline__ void store_f32(float *p, const Cols<V> &c) {
     if constexpr (V == 4)
-        *reinterpret_cast<float4 *>(p) = make_float4(c.v[0], c.v[1], c.v[2], c.v[3]);
+        store_as<f32x4, NT>(p, f32x4{c.v[0], c.v[1], c.v[2], c.v[3]});
     else
-        *p = c.v[0];
+        store_as<float, NT>(p, c.v[0]);
 }
 // bf16, rounded to nearest even by the hardware (NaN stays NaN).
 __device__ __forceinline__ uint32_t bf16_bits(float f) {
     return __builtin_bit_cast(uint16_t, static_cast<__bf16>(f));
 }
-template <int V, bool F32>
+template <int V, bool F32, bool NT = false>
 __device__ __forceinline__ void store_u(void *u, size_t i, const Cols<V> &c) {
     if constexpr (F32)
-        store_f32<V>(static_cast<float *>(u) + i, c);
+        store_f32<V, NT>(static_cast<float *>(u) + i, c);
     else if constexpr (V == 4)
-        *reinterpret_cast<uint2 *>(static_cast<uint16_t *>(u) + i) =
-            make_uint2(bf16_bits(c.v[0]) | (bf16_bits(c.v[1]) << 16),
-                       bf16_bits(c.v[2]) | (bf16_bits(c.v[3]) << 16));
+        store_as<u32x2_t, NT>(static_cast<uint16_t *>(u) + i,
+                              u32x2_t{bf16_bits(c.v[0]) | (bf16_bits(c.v[1]) << 16),
+                                      bf16_bits(c.v[2]) | (bf16_bits(c.v[3]) << 16)});
     else
-        static_cast<uint16_t *>(u)[i] = (uint16_t)bf16_bits(c.v[0]);
+        store_as<uint16_t, NT>(static_cast<uint16_t *>(u) + i, (uint16_t)bf16_bits(c.v[0]));
 }
-template <int V, bool F32>
+template <int V, bool F32, bool NT = false>
 __device__ __forceinline__ Cols<V> load_du(const void *p, size_t i) {
-    if constexpr (F32) return load_f32<V>(static_cast<const float *>(p) + i);
+    if constexpr (F32) return load_f32<V, NT>(static_cast<const float *>(p) + i);
     Cols<V> c;
     const uint16_t *q = static_cast<const uint16_t *>(p) + i;
     if constexpr (V == 4) {
-        const uint2 b = *reinterpret_cast<const uint2 *>(q);
+        const u32x2_t b = load_as<u32x2_t, NT>(q);
         c.v[0] = __uint_as_float(b.x << 16), c.v[1] = __uint_as_float(b.x & 0xFFFF0000u);
         c.v[2] = __uint_as_float(b.y << 16), c.v[3] = __uint_as_float(b.y & 0xFFFF0000u);
     } else {
-        c.v[0] = bf16_to_f32(*q);
+        c.v[0] = bf16_to_f32(load_as<uint16_t, NT>(q));
     }
     return c;
 }
@@ -122,7 +137,7 @@ struct LnParams {
 // Columns of V values in a thread's registers: N of them, column i at
 // V (thread + i * 64 WPR); one past the row's end reads the row's last one and
 // counts for nothing.
-template <int WPR, int N, int V, bool F32>
+template <int WPR, int N, int V, bool F32, bool NT>
 __global__ __launch_bounds__(WPR == 8 ? 512 : 256) void layernorm_k(LnParams P) {
     __shared__ float slot[2][WPR];
     constexpr int kRows = WPR == 1 ? 4 : 1, kTh = 64 * WPR;
@@ -150,7 +165,7 @@ __global__ __launch_bounds__(WPR == 8 ? 512 : 256) void layernorm_k(LnParams P) 
 #pragma unroll
     for (int i = 0; i < N; ++i)
         if (tid + i * kTh < n) {
-            if (P.x_out) store_f32<V>(P.x_out + row + at[i], r[i]);
+            if (P.x_out) store_f32<V, NT>(P.x_out + row + at[i], r[i]);
 #pragma unroll
             for (int j = 0; j < V; ++j) s[0] += r[i].v[j];
         }
@@ -176,7 +191,7 @@ __global__ __launch_bounds__(WPR == 8 ? 512 : 256) void layernorm_k(LnParams P) 
         if (P.b) b = load_f32<V>(P.b + at[i]);
 #pragma unroll
         for (int j = 0; j < V; ++j) r[i].v[j] = r[i].v[j] * rstd * w.v[j] + b.v[j];
-        store_u<V, F32>(P.u, row + at[i], r[i]);
+        store_u<V, F32, NT>(P.u, row + at[i], r[i]);
     }
     if (P.stats && tid == 0) {
         P.stats[2 * (size_t)t] = mu;
@@ -226,7 +241,7 @@ struct LnGradParams {
     float *part;  // [workgroups][2][d] column sums of du hat and of du, or NULL
 };
 
-template <int WPR, int N, int V, bool F32>
+template <int WPR, int N, int V, bool F32, bool NT>
 __global__ __launch_bounds__(WPR == 8 ? 512 : 256) void layernorm_grad_k(LnGradParams P) {
     constexpr int kRows = WPR == 1 ? 4 : 1, kTh = 64 * WPR;
     __shared__ float slot[2][2 * WPR];
@@ -252,12 +267,12 @@ __global__ __launch_bounds__(WPR == 8 ? 512 : 256) void layernorm_grad_k(LnGradP
         const float mu = P.stats[2 * (size_t)t], rstd = P.stats[2 * (size_t)t + 1];
         Cols<V> h[N], g[N], o[N];
 #pragma unroll
-        for (int i = 0; i < N; ++i) h[i] = load_f32<V>(P.r + row + at[i]);
+        for (int i = 0; i < N; ++i) h[i] = load_f32<V, NT>(P.r + row + at[i]);
 #pragma unroll
-        for (int i = 0; i < N; ++i) g[i] = load_du<V, F32>(P.du, row + at[i]);
+        for (int i = 0; i < N; ++i) g[i] = load_du<V, F32, NT>(P.du, row + at[i]);
         if (P.dres) {
 #pragma unroll
-            for (int i = 0; i < N; ++i) o[i] = load_f32<V>(P.dres + row + at[i]);
+            for (int i = 0; i < N; ++i) o[i] = load_f32<V, NT>(P.dres + row + at[i]);
         } else {
 #pragma unroll
             for (int i = 0; i < N; ++i)
@@ -289,7 +304,7 @@ __global__ __launch_bounds__(WPR == 8 ? 512 : 256) void layernorm_grad_k(LnGradP
             if (tid + i * kTh >= n) continue;
 #pragma unroll
             for (int j = 0; j < V; ++j) o[i].v[j] += rstd * (g[i].v[j] - m1 - h[i].v[j] * m2);
-            store_f32<V>(P.dx + row + at[i], o[i]);
+            store_f32<V, NT>(P.dx + row + at[i], o[i]);
         }
     }
     if (!P.part) return;
@@ -397,16 +412,32 @@ inline int ln_blocks(int T, int d) {
     return n < kLnBlocks ? n : kLnBlocks;
 }
 
+// Whether a call's arrays (about 14 bytes a value) do not fit `mib` of the 256
+// MiB Infinity Cache: nontemporal stores of whole vectors in the forward kernel
+// then, loads (its inputs are read for the last time) and stores in the
+// gradient's.  Forward and gradient in turn: 16384 x 4096 343 -> 317 us, 6000 x
+// 4096 137 -> 115; the gradient also where they fill half the cache, 3000 x 4096
+// 69 -> 63, but not below, 2048 x 4096 46 -> 48, 512 x 4096 23.0 -> 23.7.
+// (Nontemporal loads in the forward kernel: 166 -> 179 us alone, column by
+// column 280.)
+inline bool ln_streams(int T, int d, size_t mib) { return (size_t)T * (size_t)d * 14 > mib << 20; }
+
 template <int WPR, int N, int V, bool F32>
 void launch_ln(const LnParams &P, hipStream_t s) {
     const int rows = WPR == 1 ? 4 : 1;
-    hipLaunchKernelGGL((layernorm_k<WPR, N, V, F32>), dim3((P.T + rows - 1) / rows),
-                       dim3(WPR == 8 ? 512 : 256), 0, s, P);
+    const dim3 grid((P.T + rows - 1) / rows), block(WPR == 8 ? 512 : 256);
+    if (V == 4 && ln_streams(P.T, P.d, 256))
+        hipLaunchKernelGGL((layernorm_k<WPR, N, V, F32, V == 4>), grid, block, 0, s, P);
+    else
+        hipLaunchKernelGGL((layernorm_k<WPR, N, V, F32, false>), grid, block, 0, s, P);
 }
 template <int WPR, int N, int V, bool F32>
 void launch_ln(const LnGradParams &P, hipStream_t s) {
-    hipLaunchKernelGGL((layernorm_grad_k<WPR, N, V, F32>), dim3(ln_blocks(P.T, P.d)),
-                       dim3(WPR == 8 ? 512 : 256), 0, s, P);
+    const dim3 grid(ln_blocks(P.T, P.d)), block(WPR == 8 ? 512 : 256);
+    if (ln_streams(P.T, P.d, 128))
+        hipLaunchKernelGGL((layernorm_grad_k<WPR, N, V, F32, true>), grid, block, 0, s, P);
+    else
+        hipLaunchKernelGGL((layernorm_grad_k<WPR, N, V, F32, false>), grid, block, 0, s, P);
 }
 
 // The build for a row of d values: V = 4 needs d and every array in whole

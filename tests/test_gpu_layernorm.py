@@ -305,6 +305,43 @@ def test_offsets_past_32_bits():
     assert ((db.double() - ref).abs() <= (T / 512 + 16) * HALF * size).all()
 
 
+@pytest.mark.parametrize("T,d", [(20001, 1023), (20001, 1024), (5001, 4095), (5001, 4096),
+                                 (2501, 8190), (2501, 8192)])
+@pytest.mark.parametrize("f32", [False, True])
+def test_long_batches(T, d, f32):
+    """Calls that stream past the caches: some rows as in a call of their own, the column sums
+    against those of torch in 64 bits."""
+    import torch
+    torch.manual_seed(d)
+    kind, fl = (torch.float32, pp.PP_NORM_F32) if f32 else (torch.bfloat16, 0)
+    z = lambda *s: torch.empty(s, device="cuda")  # noqa: E731
+    x, y, dres, w = (torch.randn((T, d), device="cuda") for _ in range(4))
+    w, b = w[0].contiguous(), torch.randn(d, device="cuda")
+    du = torch.randn((T, d), device="cuda").to(kind)
+    ws = torch.empty(pp.prunepath_residual_layernorm_grad_workspace(T, d), dtype=torch.uint8,
+                     device="cuda")
+
+    def both(rows):
+        n = rows.stop - rows.start
+        xo, u, st, dx = z(n, d), torch.empty((n, d), dtype=kind, device="cuda"), z(n, 2), z(n, d)
+        dw, db = z(d), z(d)
+        # (rows of the arrays themselves where they are aligned, copies where odd rows are not)
+        a = [v[rows] if d % 4 == 0 else v[rows].clone() for v in (x, y, dres, du)]
+        pp.prunepath_residual_layernorm(a[0], a[1], xo, n, d, EPS, w, b, u, st, fl)
+        pp.prunepath_residual_layernorm_grad(xo, a[3], a[2], n, d, w, st, dx, dw, db, ws, fl)
+        return xo, u, st, dx, dw, db
+    whole = both(slice(0, T))
+    for rows in (slice(0, 3), slice(T - 5, T)):
+        for p, q in zip(whole[:4], both(rows)[:4]):
+            assert torch.equal(p[rows], q)
+    hat = (whole[0].double() - whole[2][:, :1].double()) * whole[2][:, 1:].double()
+    g = du.double()
+    c = (T / 512 + 32) * HALF
+    assert ((whole[5].double() - g.sum(0)).abs() <= c * g.abs().sum(0)).all()
+    assert ((whole[4].double() - (g * hat).sum(0)).abs() <= (c + 8 * HALF) * (g * hat).abs().sum(0) +
+            8 * HALF * g.abs().sum(0)).all()
+
+
 @pytest.mark.parametrize("d", [3, 32])
 def test_many_short_rows(d):
     T = 150001
