@@ -676,7 +676,9 @@ __global__ __launch_bounds__(64 * kTopkWaves) void route_topk_k(TopkParams P) {
         float cmax = c[0];
 #pragma unroll
         for (int q = 1; q < NQ; ++q) cmax = num.max(cmax, c[q]);
-        const float half = 0.5f * row_max(out ? -INFINITY : cmax);
+        // (the smallest float on top: half of an odd subnormal is not rounded
+        // down, which would make a distance negative)
+        const float half = fmaf(0.5f, row_max(out ? -INFINITY : cmax), 1.4e-45f);
         const float from = out ? INFINITY : half;
         uint32_t e = (uint32_t)(grp * P.Gs + sub);
 #pragma unroll

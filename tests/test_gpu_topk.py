@@ -219,6 +219,23 @@ def test_many_equal_logits(E, k, G, top, sigmoid):
             check(g, case(k, G, top, bias, 1.0, sigmoid, True, top2))
 
 
+@pytest.mark.parametrize("sigmoid", [False, True])
+def test_ends_of_the_float_range(sigmoid):
+    """Subnormal logits, logits near the largest floats, and biases of both kinds."""
+    rng = np.random.default_rng(24)
+    tiny = (rng.integers(-3, 4, (40, 64)) * 1.4e-45).astype(np.float32)
+    tiny[1] = -np.abs(tiny[1]) - np.float32(1e-40)
+    tiny[2] = np.float32(1.4e-45)
+    huge = np.float32(np.finfo(np.float32).max) * rng.uniform(-1, 1, (40, 64)).astype(np.float32)
+    huge[3, ::2], huge[3, 1::2] = np.finfo(np.float32).max, np.finfo(np.float32).min
+    big = huge[5].copy()
+    for g in (tiny, huge):
+        for bias in (None, tiny[7], big):
+            for G, top in ((1, 1), (4, 2)):
+                for top2 in (False, True):
+                    check(g, case(6, G, top, bias, 1.0, sigmoid, True, top2))
+
+
 def test_signalling_nans_take_no_part():
     g = logits(3, 40, 23)
     bits = g.view(np.uint32)
