@@ -696,7 +696,9 @@ __global__ __launch_bounds__(64 * kTopkWaves) void route_topk_k(TopkParams P) {
         return row_min(m) + last + 1u;
     };
     // A key's distance, and up to which one an entry may belong in front of
-    // it: 2^-15 of each was cut off, and c is off by err (halved like it).
+    // it: where c is exact, one of the same upper bits; else 2^-15 of each was
+    // cut off, and c is off by err (halved like it).
+    const float grow = err > 0.0f ? 1.00004f : 1.0f;
     auto distance = [](uint32_t v) { return __uint_as_float(v & 0xFFFFFF00u); };
     uint32_t last = kNone;
     float reach = 0.0f;
@@ -709,7 +711,7 @@ __global__ __launch_bounds__(64 * kTopkWaves) void route_topk_k(TopkParams P) {
         more = more && n < kFirstNone;
         const float d = distance(n);
         close |= more && j > 0 && d <= reach;
-        reach = fmaf(d, 1.0001f, err);
+        reach = fmaf(d, grow, err);
         last = n;  // past the list's end: not used any more
         len += more ? 1 : 0;
         if (c16 == 0) pk[rr * kp + j] = more ? (short)(n & 255u) : (short)-1;
