@@ -11,8 +11,9 @@
 // every sum took 910 us for both.)
 //
 // A row of up to 8192 values stays in registers between its sums and its
-// outputs: one wavefront for up to 1024 (four rows a workgroup, no barrier),
-// four for up to 4096, eight for up to 8192.  Columns are moved four at a
+// outputs: one wavefront for up to 1024 (four rows a workgroup, no barrier; two
+// forward where values are moved one at a time), four for up to 4096, eight for
+// up to 8192.  Columns are moved four at a
 // time where d and every array allow it, else one at a time.  Longer rows are
 // read again for every sum.
 // The gradient's workgroups walk over rows and keep the column sums of du hat
@@ -20,6 +21,8 @@
 // added by a second launch.
 // All sums are fp32, their order fixed by (T, d) and the kind of columns, that
 // of a row's sums by d and that alone; the partial sums are added in fp64.
+#include <type_traits>
+
 #include "pp_internal.h"
 
 namespace pp {
@@ -134,11 +137,14 @@ struct LnParams {
     float *stats;
 };
 
+// Threads of a workgroup: one row's, or four rows of a wavefront each.
+constexpr int ln_threads(int wpr) { return wpr == 1 ? 256 : 64 * wpr; }
+
 // Columns of V values in a thread's registers: N of them, column i at
 // V (thread + i * 64 WPR); one past the row's end reads the row's last one and
 // counts for nothing.
 template <int WPR, int N, int V, bool F32, bool NT>
-__global__ __launch_bounds__(WPR == 8 ? 512 : 256) void layernorm_k(LnParams P) {
+__global__ __launch_bounds__(ln_threads(WPR)) void layernorm_k(LnParams P) {
     __shared__ float slot[2][WPR];
     constexpr int kRows = WPR == 1 ? 4 : 1, kTh = 64 * WPR;
     const int tid = WPR == 1 ? threadIdx.x & 63 : threadIdx.x;
@@ -242,7 +248,7 @@ struct LnGradParams {
 };
 
 template <int WPR, int N, int V, bool F32, bool NT>
-__global__ __launch_bounds__(WPR == 8 ? 512 : 256) void layernorm_grad_k(LnGradParams P) {
+__global__ __launch_bounds__(ln_threads(WPR)) void layernorm_grad_k(LnGradParams P) {
     constexpr int kRows = WPR == 1 ? 4 : 1, kTh = 64 * WPR;
     __shared__ float slot[2][2 * WPR];
     __shared__ float join[WPR == 1 ? 3 * 2 * N * V * 64 : 1];
@@ -425,7 +431,7 @@ inline bool ln_streams(int T, int d, size_t mib) { return (size_t)T * (size_t)d 
 template <int WPR, int N, int V, bool F32>
 void launch_ln(const LnParams &P, hipStream_t s) {
     const int rows = WPR == 1 ? 4 : 1;
-    const dim3 grid((P.T + rows - 1) / rows), block(WPR == 8 ? 512 : 256);
+    const dim3 grid((P.T + rows - 1) / rows), block(ln_threads(WPR));
     if (V == 4 && ln_streams(P.T, P.d, 256))
         hipLaunchKernelGGL((layernorm_k<WPR, N, V, F32, V == 4>), grid, block, 0, s, P);
     else
@@ -433,7 +439,7 @@ void launch_ln(const LnParams &P, hipStream_t s) {
 }
 template <int WPR, int N, int V, bool F32>
 void launch_ln(const LnGradParams &P, hipStream_t s) {
-    const dim3 grid(ln_blocks(P.T, P.d)), block(WPR == 8 ? 512 : 256);
+    const dim3 grid(ln_blocks(P.T, P.d)), block(ln_threads(WPR));
     if (ln_streams(P.T, P.d, 128))
         hipLaunchKernelGGL((layernorm_grad_k<WPR, N, V, F32, true>), grid, block, 0, s, P);
     else
@@ -445,12 +451,16 @@ void launch_ln(const LnGradParams &P, hipStream_t s) {
 template <int V, bool F32, typename Params>
 void launch_ln_width(const Params &P, hipStream_t s) {
     constexpr int q = 4 / V;  // registers' columns per float4
+    // two wavefronts a row where one would hold 9 to 16 single values a lane
+    // (d 1023: one row 5.4 -> 4.1 us, d 771: 1001 rows 6.1 -> 5.2, 16384 rows
+    // 35.9 -> 31.9); the gradient's partial rows would double
+    constexpr bool two = V == 1 && std::is_same_v<Params, LnParams>;
     if (P.d <= 256)
         launch_ln<1, 1 * q, V, F32>(P, s);
     else if (P.d <= 512)
         launch_ln<1, 2 * q, V, F32>(P, s);
     else if (P.d <= 1024)
-        launch_ln<1, 4 * q, V, F32>(P, s);
+        launch_ln<two ? 2 : 1, two ? 8 : 4 * q, V, F32>(P, s);
     else if (P.d <= 2048)
         launch_ln<4, 2 * q, V, F32>(P, s);
     else if (P.d <= 4096)
