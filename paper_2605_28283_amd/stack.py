@@ -46,6 +46,8 @@ class DecodeStack:
             if len(self.topk["sel_bias"]) != self.L:
                 raise ValueError("topk: %d selection biases for %d layers"
                                  % (len(self.topk["sel_bias"]), self.L))
+            if any(b is not None and b.numel() != E for b in self.topk["sel_bias"]):
+                raise ValueError("topk: a selection bias that is not [%d]" % E)
         import torch
         dev = "cuda"
         self.x_in = torch.zeros((T, d), dtype=torch.float32, device=dev)

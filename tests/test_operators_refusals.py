@@ -3,6 +3,7 @@ the residual layer norm: every call here returns before any HIP call (runs witho
 fp64 forms that the GPU tests compare with are pinned here too, by brute force and differences."""
 import numpy as np
 import pytest
+import torch
 
 import paper_2605_28283_amd as pp
 from oracle import operators as op
@@ -100,6 +101,13 @@ def test_stack_refuses():
         DecodeStack([1, 2], 64, 2, 1, 0.5, topk=dict(n_groups=2))
     with pytest.raises(ValueError):
         DecodeStack([1, 2], 64, 2, 1, 0.5, topk=dict(k=1, sel_bias=[None]))
+
+
+def test_stack_refuses_short_selection_bias():
+    with pytest.raises(ValueError):
+        DecodeStack([1, 2], 64, 2, 1, 0.5, topk=dict(k=1, sel_bias=[None, torch.zeros(3)]))
+    with pytest.raises(ValueError):
+        DecodeStack([1], 64, 2, 1, 0.5, topk=dict(k=1, sel_bias=[torch.zeros(1)]))
 
 
 # ------------------------------------------------------------------ the fp64 forms
