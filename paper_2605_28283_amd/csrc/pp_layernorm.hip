@@ -452,7 +452,7 @@ template <int V, bool F32, typename Params>
 void launch_ln_width(const Params &P, hipStream_t s) {
     constexpr int q = 4 / V;  // registers' columns per float4
     // two wavefronts a row where one would hold 9 to 16 single values a lane
-    // (d 1023: one row 5.4 -> 4.1 us, d 771: 1001 rows 6.1 -> 5.2, 16384 rows
+    // (d 1023: one row 5.4 -> 4.2 us, d 771: 1001 rows 6.1 -> 5.2, 16384 rows
     // 35.9 -> 31.9); the gradient's partial rows would double
     constexpr bool two = V == 1 && std::is_same_v<Params, LnParams>;
     if (P.d <= 256)
