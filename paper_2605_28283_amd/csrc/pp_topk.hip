@@ -628,10 +628,12 @@ __global__ __launch_bounds__(64 * kTopkWaves) void route_topk_k(TopkParams P) {
         if (P.lanes > 1) join(row_lane<kX1>(a), row_lane<kX1>(n));
         if (P.lanes > 2) join(row_lane<kX2>(a), row_lane<kX2>(n));
         if (P.lanes > 4) join(row_lane<kX4>(a), row_lane<kX4>(n));
-        const float v = top2 && n > -INFINITY ? a + n : a;
+        // worths of two scores are halved (the sum of two floats may be past the
+        // largest): -inf is a group of no experts and nothing else
+        const float v = top2 ? fmaf(0.5f, n > -INFINITY ? n : 0.0f, 0.5f * a) : a;
         // groups in front, and those that might be if each worth is off by
         // what its two scores and their sum are
-        const float off = SCORES ? 3.0f * err : 0.0f;
+        const float off = SCORES ? (top2 ? 1.5f : 3.0f) * err : 0.0f;
         int front = 0, near = 0;
         each_rotation([&](auto ctrl) {
             constexpr int R = decltype(ctrl)::value & 15;
