@@ -186,6 +186,18 @@ __device__ __forceinline__ double sigmoid64(float z) {
     const double e = exp_neg(-fabs((double)z)), r = rcp64(1.0 + e);
     return z >= 0.0f ? r : e * r;
 }
+// A score and c in 64 bits, each step rounded (no product is fused into a sum),
+// from 1 / (sum of e^(z - zmax)) added up by expert (exact_softmax_scale):
+// the same bits wherever they are formed, so that c's next to each other are
+// in one order in every kernel.
+__device__ __forceinline__ double score64(bool sig, float z, float zmax, double scale) {
+#pragma clang fp contract(off)
+    return sig ? sigmoid64(z) : exp_neg((double)z - (double)zmax) * scale;
+}
+__device__ __forceinline__ double biased64(double s, float b) {
+#pragma clang fp contract(off)
+    return s + (double)b;
+}
 // sigmoid(z) over e^m for m = min(largest z, 0): relative scores that do not
 // all underflow.
 __device__ __forceinline__ float rel_sigmoid(float z, float m) {
@@ -303,7 +315,8 @@ __device__ __forceinline__ int groups_in_front(const TopkParams &P, double a, do
     return front;
 }
 
-// 1 / (sum of e^(z - zmax)) of a row in 64 bits, by the whole wavefront.
+// 1 / (sum of e^(z - zmax)) of a row in 64 bits, by the whole wavefront: lane l
+// adds those of experts l, l + 64, ..., then pairs of lanes.
 __device__ __forceinline__ double exact_softmax_scale(const TopkParams &P, const float *zr,
                                                       float zmax, int lane) {
     double S = 0.0;
@@ -317,9 +330,8 @@ __device__ __forceinline__ double exact_softmax_scale(const TopkParams &P, const
 }
 
 // The groups of a row that stay, by scores in 64 bits: bit g << (lanes_log + 2)
-// for group g.  For a call with a bias, or worth two scores without one
-// (whose softmax scores need no sum for that: scale 1).  zr, zb: the row and
-// the bias.
+// for group g.  For a call with a bias, or worth two scores without one.
+// zr, zb: the row and the bias.
 __device__ __forceinline__ unsigned long long exact_groups(const TopkParams &P, const float *zr,
                                                            const float *zb, float zmax,
                                                            double scale, int lane) {
@@ -331,8 +343,7 @@ __device__ __forceinline__ unsigned long long exact_groups(const TopkParams &P, 
         for (int i = lane & ((1 << wl) - 1); i < P.Gs; i += 1 << wl) {
             const float z = zr[grp * P.Gp + i];
             const float b = P.sel_bias ? zb[grp * P.Gp + i] : 0.0f;
-            double v = sig ? sigmoid64(z) : exp_neg((double)z - (double)zmax) * scale;
-            v += (double)b;
+            const double v = biased64(score64(sig, z, zmax, scale), b);
             if (z > -INFINITY && b > -INFINITY) {
                 n = fmax(n, fmin(a, v));
                 a = fmax(a, v);
@@ -382,14 +393,14 @@ __device__ __forceinline__ void choose_row(const TopkParams &P, const float *zr,
         S = wave_reduce(S, lane, [](double a, double b) { return a + b; });
         const double r = S > 0.0 ? rcp64(S) : 0.0;
 #pragma unroll
-        for (int q = 0; q < NE; ++q) s[q] *= r;
+        for (int q = 0; q < NE; ++q) s[q] *= r;  // as in score64
     }
 #pragma unroll
     for (int q = 0; q < NE; ++q) {
         const int e = lane + 64 * q;
         if (P.sel_bias) {
             const float b = e < P.E ? zb[topk_place(P, e)] : -INFINITY;
-            const double v = s[q] + (double)b;
+            const double v = biased64(s[q], b);
             c[q] = c[q] > -INFINITY && b > -INFINITY ? v : -INFINITY;
         }
         // without a bias experts are in the order of the logits
@@ -657,7 +668,7 @@ __global__ __launch_bounds__(64 * kTopkWaves) void route_topk_k(TopkParams P) {
                     if (!((open >> (16 * r)) & 0xFFFFull)) continue;
                     const float top = __shfl(zmax, 16 * r, 64);
                     const double scale =
-                        biased && !sig ? exact_softmax_scale(P, zs + r * P.Rp, top, lane) : 1.0;
+                        sig ? 1.0 : exact_softmax_scale(P, zs + r * P.Rp, top, lane);
                     const unsigned long long stay =
                         exact_groups(P, zs + r * P.Rp, zb, top, scale, lane);
                     if (rr == r) out = !((stay >> (grp << (P.lanes_log + 2))) & 1ull);
@@ -750,9 +761,7 @@ __global__ __launch_bounds__(64 * kTopkWaves) void route_topk_k(TopkParams P) {
                 const int e = pk[r * kp + lane], at = topk_place(P, e);
                 const float x = zs[r * P.Rp + at];
                 double v = (double)x;
-                if (biased)
-                    v = (sig ? sigmoid64(x) : exp_neg((double)x - (double)top) * scale) +
-                        (double)zb[at];
+                if (biased) v = biased64(score64(sig, x, top, scale), zb[at]);
                 worth[e] = v;
             }
             sort_list(worth, pk + r * kp, n, k, lane);
@@ -845,17 +854,28 @@ __global__ __launch_bounds__(64 * kTopkWaves) void route_topk_wide_k(TopkParams 
                 by[q] = z[q] >= 0.0f ? d : by[q] * d;
             }
         } else {
+            if (P.n_groups > 1) {  // added up by expert (in one group S has that order)
+#pragma unroll
+                for (int q = 0; q < NQ; ++q)
+                    if (q << wl < held) cs[e0 + (q << wl)] = by[q];
+                wave_sync();
+                S = 0.0;
+#pragma unroll
+                for (int q = 0; q < kMaxExperts / 64; ++q)
+                    if (lane + 64 * q < E) S += cs[lane + 64 * q];
+                wave_sync();
+            }
             S = wave_reduce(S, lane, [](double a, double b) { return a + b; });
             const double r = S > 0.0 ? rcp64(S) : 0.0;
 #pragma unroll
-            for (int q = 0; q < NQ; ++q) by[q] *= r;
+            for (int q = 0; q < NQ; ++q) by[q] *= r;  // as in score64
         }
     }
     if (biased) {
 #pragma unroll
         for (int q = 0; q < NQ; ++q) {
             const float b = zb[q << wl < held ? e0 + (q << wl) : 0];
-            c[q] = z[q] > -INFINITY && b > -INFINITY ? by[q] + (double)b : -INFINITY;
+            c[q] = z[q] > -INFINITY && b > -INFINITY ? biased64(by[q], b) : -INFINITY;
         }
     }
     if (P.n_groups > 1) {

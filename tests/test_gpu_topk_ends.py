@@ -4,7 +4,7 @@ largest float, weights of logits at the ends of the float range."""
 import numpy as np
 import pytest
 
-from test_gpu_topk import case, check
+from test_gpu_topk import case, check, route
 
 pytestmark = pytest.mark.gpu
 
@@ -30,3 +30,43 @@ def test_group_worths_past_the_largest_float(sigmoid):
         for top in (1, 2, 3):
             for top2 in (True, False):
                 check(g, case(2, 4, top, bias, 1.0, sigmoid, True, top2))
+
+
+def test_groups_that_only_normalised_scores_tell_apart():
+    """1 + e^-37 is 1 in 64 bits, a third of it is one step above a third."""
+    g = np.full((1, 256), -np.inf, np.float32)
+    g[0, [0, 32, 64]] = 0.0
+    g[0, [1, 33, 65]] = [-60.0, -37.0, -60.0]
+    idx, _ = check(g, case(2, 8, 1, None, 1.0, False, False, True))
+    assert idx.tolist() == [[32, 33]]
+
+
+@pytest.mark.parametrize("biased", [False, True])
+@pytest.mark.parametrize("sigmoid", [False, True])
+@pytest.mark.parametrize("G,top,top2", [(8, 8, False), (8, 3, True), (1, 1, False)])
+def test_the_number_of_tokens_does_not_change_the_choice(biased, sigmoid, G, top, top2):
+    """c's that differ by the last bits of 64: scores next to each other beside a bias of 1 (whose
+    64-bit neighbours are 2^-52 apart), or groups worth nearly the same.  The rows one by one, in
+    batches of a thousand and all at once get the same experts."""
+    T, E, k = 20000, 256, 8
+    rng = np.random.default_rng(G + 2 * sigmoid)
+    g = rng.standard_normal((T, E)).astype(np.float32)
+    near = np.arange(3, E, 16)
+    bias = None
+    if biased:
+        bias = np.zeros(E, np.float32)
+        bias[near] = 1.0
+        g[:, near] = -(rng.random((T, len(near))) * 8e-15).astype(np.float32)
+    else:
+        g -= 45.0
+        g[:, near[::2]] = 0.0
+        g[:, near[1::2]] = -(36.0 + 2.0 * rng.random((T, len(near) // 2))).astype(np.float32)
+    c = case(k, G, top, bias, 1.0, sigmoid, True, top2)
+    idx, w = route(g, c)
+    for t in range(0, T, 1000):
+        i2, w2 = route(g[t:t + 1000], c)
+        np.testing.assert_array_equal(i2, idx[t:t + 1000])
+        np.testing.assert_array_equal(w2, w[t:t + 1000])
+    for t in range(0, T, 4001):
+        i1, _ = route(g[t:t + 1], c)
+        np.testing.assert_array_equal(i1[0], idx[t])
