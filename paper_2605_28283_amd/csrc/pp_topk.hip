@@ -484,15 +484,21 @@ __device__ __forceinline__ void store_row(const TopkParams &P, const float *zr, 
                 tot += sig ? rel_sigmoid(x, m) : expf(x - m);
             }
         }
-        // every 16 lanes take all slots, in the same order for either W
-        scale = P.scale / row_sum(tot);  // rows of empty slots do not use it
+        // every 16 lanes take all slots, in the same order for either W.  Over
+        // twice the sum (which is 1/2 or more), and scores twice below: a scale
+        // near the largest float stays one.  Rows of empty slots do not use it.
+        scale = P.scale / (2.0f * row_sum(tot));
     }
     for (int j = l; j < k; j += W) {
         const int e = list[j];
         float w = 0.0f;
         if (e >= 0) {
             const float x = zr[topk_place(P, e)];
-            w = scale * (sig ? rel_sigmoid(x, m) : expf(x - m));
+            w = sig ? rel_sigmoid(x, m) : expf(x - m);
+            // (the quotient's rounding alone may pass the largest float)
+            w = P.flags & PP_TOPK_RENORM
+                    ? __builtin_amdgcn_fmed3f(scale * (2.0f * w), -kFltMax, kFltMax)
+                    : scale * w;
         }
         P.idx[(size_t)t * k + j] = e;
         P.w[(size_t)t * k + j] = w;

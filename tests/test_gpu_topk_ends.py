@@ -4,7 +4,8 @@ largest float, weights of logits at the ends of the float range."""
 import numpy as np
 import pytest
 
-from test_gpu_topk import case, check, route
+from oracle import operators as op
+from test_gpu_topk import STEP, case, check, route
 
 pytestmark = pytest.mark.gpu
 
@@ -70,3 +71,48 @@ def test_the_number_of_tokens_does_not_change_the_choice(biased, sigmoid, G, top
     for t in range(0, T, 4001):
         i1, _ = route(g[t:t + 1], c)
         np.testing.assert_array_equal(i1[0], idx[t])
+
+
+def weight_tolerance(g, idx, c):
+    """As in test_gpu_topk, 16 roundings and |x| 2^-24 of an exponent's argument x, counted where
+    it shows: x = z - m of the expert itself, m its row's (renormalised: the chosen ones') largest
+    logit; the terms of the sum have a mean |x| of at most log 256 < 6.  Where x < -104 the weight
+    is below every float."""
+    z = np.clip(np.nan_to_num(g.astype(np.float64), nan=-np.inf, posinf=FLT_MAX), -np.inf, FLT_MAX)
+    zc = np.where(idx >= 0, np.take_along_axis(z, np.maximum(idx, 0).astype(np.int64), 1), -np.inf)
+    m = (zc if c["renorm"] else z).max(1, keepdims=True)
+    if c["sigmoid"]:
+        m = np.minimum(m, 0.0) if c["renorm"] else 0.0
+        zc = np.minimum(zc, 0.0)
+    with np.errstate(invalid="ignore"):
+        x = np.minimum(np.nan_to_num(np.abs(zc - m), nan=0.0, posinf=104.0), 104.0)
+    return (22 + x) * STEP
+
+
+def check_weights(g, c):
+    ref_i, ref_w = op.route_topk(g, **c)
+    for reps in (1, 4100 // len(g) + 1):
+        idx, w = route(np.tile(g, (reps, 1)), c)
+        np.testing.assert_array_equal(idx, np.tile(ref_i, (reps, 1)))
+        ref = np.tile(ref_w, (reps, 1))
+        tol = np.tile(weight_tolerance(g, ref_i, c), (reps, 1)) * np.abs(ref)
+        # (below the smallest normal float a weight may be flushed)
+        assert (np.abs(w - ref) <= tol + 1.2e-38 * max(1.0, abs(c["scale"]))).all()
+
+
+def scaled(sigmoid, renorm, E, scales):
+    rng = np.random.default_rng(E)
+    g = (rng.standard_normal((40, E)) * 2).astype(np.float32)
+    g[0], g[1], g[2] = 0.0, -30.0, 30.0
+    g[3], g[3, 7] = -np.inf, -0.1
+    for scale in scales:
+        for k in (1, 3):
+            check_weights(g, case(k, 1, 1, None, scale, sigmoid, renorm))
+
+
+@pytest.mark.parametrize("sigmoid", [False, True])
+@pytest.mark.parametrize("renorm", [False, True])
+@pytest.mark.parametrize("E", [24, 256])
+def test_large_scales(sigmoid, renorm, E):
+    """No weight passes the largest float where scale does not."""
+    scaled(sigmoid, renorm, E, (3.0e38, -3.0e38, 1.9e38, 1e-30))
