@@ -410,6 +410,7 @@ __global__ __launch_bounds__(1024) void layernorm_sum_k(const float *__restrict_
 }
 
 constexpr int kLnMaxRows = 1 << 20, kLnMaxWidth = 1 << 16;
+constexpr float kLnMaxEps = 3.402823466e38f;  // any float
 
 // Gradient workgroups (and partial rows): one for each four rows or each row,
 // up to kLnBlocks.
@@ -492,7 +493,7 @@ extern "C" pp_status prunepath_residual_layernorm(const float *x, const float *y
     if (!x || !u) return PP_EINVAL;
     if (T < 1 || T > kLnMaxRows || d < 1 || d > kLnMaxWidth || (flags & ~PP_NORM_F32))
         return PP_EINVAL;
-    if (!(eps >= 0.0f && eps <= 3.0e38f)) return PP_EINVAL;  // also rejects NaN
+    if (!(eps >= 0.0f && eps <= kLnMaxEps)) return PP_EINVAL;  // also rejects NaN
     const bool f32 = (flags & PP_NORM_F32) != 0;
     if ((((uintptr_t)x | (uintptr_t)y | (uintptr_t)x_out | (uintptr_t)w | (uintptr_t)b |
           (uintptr_t)stats) & 3) || ((uintptr_t)u & (f32 ? 3 : 1)))

@@ -1150,7 +1150,7 @@ pp_status check_rule(int32_t E, int32_t k, int32_t n_groups, int32_t top_groups,
     if (!idx || !w || (const void *)idx == (const void *)w) return PP_EINVAL;
     if (((uintptr_t)idx | (uintptr_t)w | (uintptr_t)sel_bias) & 3) return PP_EINVAL;
     if (flags & ~kRuleFlags) return PP_EINVAL;
-    if (!(fabsf(scale) <= 3.0e38f)) return PP_EINVAL;  // also rejects NaN
+    if (!(fabsf(scale) <= kFltMax)) return PP_EINVAL;  // also rejects NaN
     if (n_groups < 1 || E % n_groups != 0 || top_groups < 1 || top_groups > n_groups)
         return PP_EINVAL;
     if (k < 1 || k > top_groups * (E / n_groups)) return PP_EINVAL;
@@ -1274,7 +1274,7 @@ extern "C" pp_status prunepath_route_topk_grad(const float *g, int32_t T, int32_
         return PP_EINVAL;
     if (T < 1 || T > kMaxTopkRows || E < 1 || E > kMaxExperts || k < 1 || k > E) return PP_EINVAL;
     if (flags & ~(kRuleFlags | PP_GRAD_ADD)) return PP_EINVAL;
-    if (!(fabsf(scale) <= 3.0e38f)) return PP_EINVAL;
+    if (!(fabsf(scale) <= kFltMax)) return PP_EINVAL;
     const TopkGradParams P = {g, T, E, k, expert_idx, dgate_w, scale, flags, dg};
     launch_topk_grad(P, static_cast<hipStream_t>(hip_stream));
     return hipGetLastError() == hipSuccess ? PP_OK : PP_EHIP;
