@@ -6,11 +6,72 @@ import pytest
 
 import paper_2605_28283_amd as pp
 from oracle import operators as op
-from test_gpu_topk import STEP, case, dev, flags_of, route
+from test_gpu_topk import STEP, case, check, dev, flags_of, route
 
 pytestmark = pytest.mark.gpu
 
 FLT_MAX = float(np.finfo(np.float32).max)
+
+
+@pytest.mark.parametrize("sigmoid", [False, True])
+def test_group_worths_past_the_largest_float(sigmoid):
+    """Two biases of a group add up to more than any float, of either sign: such a group holds
+    experts like any other, and its worth is compared as it is."""
+    f = lambda a: np.array(a, np.float32)  # noqa: E731
+    biases = [(16, f([-2e38] + [-3.3e38] * 3 + [-2.1e38] * 2 + [-3e38] * 2 + [-3e38] * 8)),
+              (16, f([3e38, 2e38] * 2 + [2.6e38] * 4 + [3.3e38, 1.5e38] * 2 + [2e38] * 4)),
+              (64, np.full(64, -FLT_MAX, np.float32)), (64, np.full(64, FLT_MAX, np.float32)),
+              (64, np.where(np.arange(64) % 16 < 15, -FLT_MAX, 0.25).astype(np.float32)),
+              (64, np.where(np.arange(64) < 20, 0.125, -FLT_MAX).astype(np.float32)),
+              (256, np.where(np.arange(256) < 70, 0.125, -FLT_MAX).astype(np.float32))]
+    for E, bias in biases:
+        g = np.random.default_rng(E).standard_normal((5, E)).astype(np.float32)
+        g[0] = 0.0
+        g[1, E // 4:E // 2] = -np.inf                      # a group without experts
+        g[2, :E // 4 - 1] = -np.inf                        # one of a single expert
+        for top in (1, 2, 3):
+            for top2 in (True, False):
+                check(g, case(2, 4, top, bias, 1.0, sigmoid, True, top2))
+
+
+def test_groups_that_only_normalised_scores_tell_apart():
+    """1 + e^-37 is 1 in 64 bits, a third of it is one step above a third."""
+    g = np.full((1, 256), -np.inf, np.float32)
+    g[0, [0, 32, 64]] = 0.0
+    g[0, [1, 33, 65]] = [-60.0, -37.0, -60.0]
+    idx, _ = check(g, case(2, 8, 1, None, 1.0, False, False, True))
+    assert idx.tolist() == [[32, 33]]
+
+
+@pytest.mark.parametrize("biased", [False, True])
+@pytest.mark.parametrize("sigmoid", [False, True])
+@pytest.mark.parametrize("G,top,top2", [(8, 8, False), (8, 3, True), (1, 1, False)])
+def test_the_number_of_tokens_does_not_change_the_choice(biased, sigmoid, G, top, top2):
+    """c's that differ by the last bits of 64: scores next to each other beside a bias of 1 (whose
+    64-bit neighbours are 2^-52 apart), or groups worth nearly the same.  The rows one by one, in
+    batches of a thousand and all at once get the same experts."""
+    T, E, k = 20000, 256, 8
+    rng = np.random.default_rng(G + 2 * sigmoid)
+    g = rng.standard_normal((T, E)).astype(np.float32)
+    near = np.arange(3, E, 16)
+    bias = None
+    if biased:
+        bias = np.zeros(E, np.float32)
+        bias[near] = 1.0
+        g[:, near] = -(rng.random((T, len(near))) * 8e-15).astype(np.float32)
+    else:
+        g -= 45.0
+        g[:, near[::2]] = 0.0
+        g[:, near[1::2]] = -(36.0 + 2.0 * rng.random((T, len(near) // 2))).astype(np.float32)
+    c = case(k, G, top, bias, 1.0, sigmoid, True, top2)
+    idx, w = route(g, c)
+    for t in range(0, T, 1000):
+        i2, w2 = route(g[t:t + 1000], c)
+        np.testing.assert_array_equal(i2, idx[t:t + 1000])
+        np.testing.assert_array_equal(w2, w[t:t + 1000])
+    for t in range(0, T, 4001):
+        i1, _ = route(g[t:t + 1], c)
+        np.testing.assert_array_equal(i1[0], idx[t])
 
 
 def weight_tolerance(g, idx, c):
@@ -38,6 +99,23 @@ def check_weights(g, c):
         tol = np.tile(weight_tolerance(g, ref_i, c), (reps, 1)) * np.abs(ref)
         # (below the smallest normal float a weight may be flushed)
         assert (np.abs(w - ref) <= tol + 1.2e-38 * max(1.0, abs(c["scale"]))).all()
+
+
+@pytest.mark.parametrize("sigmoid", [False, True])
+@pytest.mark.parametrize("renorm", [False, True])
+def test_weights_at_the_ends_of_the_float_range(sigmoid, renorm):
+    rng = np.random.default_rng(31)
+    g = np.float32(FLT_MAX) * rng.uniform(-1, 1, (12, 64)).astype(np.float32)
+    g[1, ::2], g[1, 1::2] = FLT_MAX, -FLT_MAX
+    g[2], g[3] = -FLT_MAX, FLT_MAX
+    g[4], g[4, [5, 6, 40]] = -FLT_MAX, [0.0, 1.0, -2.0]
+    g[5], g[5, 9] = 0.0, FLT_MAX
+    g[6] = (rng.integers(-3, 4, 64) * 1.4e-45).astype(np.float32)
+    g[7], g[7, 3:7] = -np.inf, [-FLT_MAX, FLT_MAX, np.inf, np.nan]
+    g[8] = rng.uniform(-120, 0, 64)
+    for bias in (None, rng.uniform(-0.2, 0.2, 64).astype(np.float32)):
+        for G, top in ((1, 1), (4, 2)):
+            check_weights(g, case(6, G, top, bias, 1.0, sigmoid, renorm))
 
 
 def scaled(sigmoid, renorm, E, scales):
