@@ -251,7 +251,8 @@ pp_status prunepath_route_topk_grad(const float *g, int32_t T, int32_t E, int32_
  *                weights
  *   gate_w     : [T, k] fp32 or NULL (weights 1); any values.  They scale the
  *                experts' hidden values, as PP_AGG_SIGMOID's gates do; the
- *                handle's own rule and aggregation play no part
+ *                handle's own rule and aggregation play no part.  A NaN or an
+ *                infinity makes its token's y row NaN, and no other one
  *   y          : [T, d] fp32 out, overwritten
  * Decode is for small batches (slices of 64 tokens), prefill for long ones, as
  * with prunepath_ffn_decode and prunepath_ffn_prefill, whose summation orders

@@ -6,7 +6,9 @@
 // and the weight of each kept (token, expert) pair, which scales h before it
 // is rounded.
 // A slot outside 0 .. E - 1 is empty; an expert named twice by a token counts
-// once with the sum of its weights, added in slot order.
+// once with the sum of its weights, added in slot order.  A weight that is a
+// NaN becomes the plain one: h is split into two bf16 numbers by adding to its
+// bits, which carries a NaN of all ones over into a zero.
 #include "pp_internal.h"
 
 namespace pp {
@@ -30,9 +32,10 @@ __device__ __forceinline__ void scatter_tokens(const RoutedParams &P, int t0, in
     const float *w = P.w ? P.w + (size_t)t0 * P.k : nullptr;
     float *gs = P.gsig + (size_t)t0 * P.E;
     const int slots = n * P.k, th = (int)blockDim.x;
+    auto plain = [](float v) { return v == v ? v : __builtin_nanf(""); };
     auto store = [&](int s, int e, float v) {
         const int t = s / P.k;
-        if ((unsigned)e < (unsigned)P.E && !twice[t]) gs[(size_t)t * P.E + e] = v;
+        if ((unsigned)e < (unsigned)P.E && !twice[t]) gs[(size_t)t * P.E + e] = plain(v);
     };
     const int s0 = (int)threadIdx.x;
     const int e0 = s0 < slots ? idx[s0] : -1;
@@ -55,7 +58,7 @@ __device__ __forceinline__ void scatter_tokens(const RoutedParams &P, int t0, in
         for (int j = 0; j < P.k; ++j) {
             const int e = idx[t * P.k + j];
             if ((unsigned)e < (unsigned)P.E)
-                gs[(size_t)t * P.E + e] += w ? w[t * P.k + j] : 1.0f;
+                gs[(size_t)t * P.E + e] += w ? plain(w[t * P.k + j]) : 1.0f;
         }
     }
 }
