@@ -182,6 +182,14 @@ def _arg(a, kind, n, name, dev):
     raise ValueError("%s: %d elements, the call needs %d" % (name, a.numel(), n))
 
 
+_dims = {}  # (d, E) of the handles made here: what the calls on them touch
+
+
+def _sizes(handle):
+    """(d, E) of a handle; zeros, which ask nothing of an array, for one made elsewhere."""
+    return _dims.get(handle, (0, 0))
+
+
 _current = None  # (current device's index, its current stream's handle by index)
 
 
@@ -234,6 +242,7 @@ def prunepath_create(d, d_ff, E, max_tokens, W_r, W_gate, W_up, W_down, perm=Non
                                  _ptr(W_down, "bf16"), _ptr(perm, "i32"),
                                  _ptr(router_bias, "f32"), flags, _stream(stream))
     _check(st, "prunepath_create")
+    _dims[out.value] = (d, E)
     return out.value
 
 
@@ -246,6 +255,7 @@ def prunepath_create_mlp(d, d_ff, E, max_tokens, W_r, W_fc, b_fc, W_proj, b_proj
                                      _ptr(W_proj, "bf16"), _ptr(b_proj, "f32"), _ptr(perm, "i32"),
                                      _ptr(router_bias, "f32"), flags, _stream(stream))
     _check(st, "prunepath_create_mlp")
+    _dims[out.value] = (d, E)
     return out.value
 
 
@@ -281,12 +291,12 @@ def prunepath_residual_rmsnorm(x, y, x_out, T, d, eps, u=None, stream=None):
 def prunepath_route_topk(handle, x, T, inv_temp, k, n_groups, top_groups, sel_bias, scale, flags,
                          expert_idx, gate_w, logits=None, stream=None):
     """k experts per token by the handle's router (include/prunepath.h has the rule)."""
-    v, stream = _place(stream)
+    (v, stream), (d, E) = _place(stream), _sizes(handle)
     st = load().prunepath_route_topk(
-        handle, _arg(x, "bf16", 0, "x", v), T, _arg(inv_temp, "f32", T, "inv_temp", v), k,
-        n_groups, top_groups, _arg(sel_bias, "f32", 0, "sel_bias", v), scale, flags,
+        handle, _arg(x, "bf16", T * d, "x", v), T, _arg(inv_temp, "f32", T, "inv_temp", v), k,
+        n_groups, top_groups, _arg(sel_bias, "f32", E, "sel_bias", v), scale, flags,
         _arg(expert_idx, "i32", T * k, "expert_idx", v), _arg(gate_w, "f32", T * k, "gate_w", v),
-        _arg(logits, "f32", 0, "logits", v), stream)
+        _arg(logits, "f32", T * E, "logits", v), stream)
     _check(st, "prunepath_route_topk")
 
 
@@ -313,11 +323,11 @@ def prunepath_route_topk_grad(g, T, E, k, expert_idx, dgate_w, scale, flags, dg,
 
 
 def _ffn_routed(name, handle, x, T, k, expert_idx, gate_w, y, stream):
-    v, stream = _place(stream)
-    st = getattr(load(), name)(handle, _arg(x, "bf16", 0, "x", v), T, k,
+    (v, stream), (d, _) = _place(stream), _sizes(handle)
+    st = getattr(load(), name)(handle, _arg(x, "bf16", T * d, "x", v), T, k,
                                _arg(expert_idx, "i32", T * k, "expert_idx", v),
-                               _arg(gate_w, "f32", T * k, "gate_w", v), _arg(y, "f32", 0, "y", v),
-                               stream)
+                               _arg(gate_w, "f32", T * k, "gate_w", v),
+                               _arg(y, "f32", T * d, "y", v), stream)
     _check(st, name)
 
 
@@ -420,4 +430,5 @@ def prunepath_profile_end(handle):
 
 def prunepath_destroy(handle):
     if handle:
+        _dims.pop(handle, None)
         load().prunepath_destroy(handle)
