@@ -190,6 +190,7 @@ pp_status prunepath_ffn_prefill(pp_layer *L, const uint16_t *x, int32_t T, float
  *   expert_idx : [T, k] int32; row t holds the chosen experts in descending
  *                order of c, then -1 where fewer than k can be chosen
  *   gate_w     : [T, k] fp32, the weights of the same slots, 0 in empty ones
+ * An output may alias no other array (PP_EINVAL where two are the same).
  * Results do not depend on T or on the other tokens.  Nothing is allocated
  * and nothing but the outputs (and the handle's router scratch) is written, so
  * the calls may be captured; those without a handle may run at the same time

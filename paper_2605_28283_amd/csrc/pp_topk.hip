@@ -1144,10 +1144,14 @@ void launch_topk_grad(const TopkGradParams &P, hipStream_t s) {
 
 constexpr uint32_t kRuleFlags = PP_SCORE_SIGMOID | PP_TOPK_RENORM | PP_GROUP_TOP2;
 
-pp_status check_rule(int32_t E, int32_t k, int32_t n_groups, int32_t top_groups,
+// in: the logits, or the tokens.  (A wavefront's outputs are other wavefronts'
+// inputs if they share an array.)
+pp_status check_rule(const void *in, int32_t E, int32_t k, int32_t n_groups, int32_t top_groups,
                      const float *sel_bias, float scale, uint32_t flags, const int32_t *idx,
                      const float *w) {
     if (!idx || !w || (const void *)idx == (const void *)w) return PP_EINVAL;
+    if (in == (const void *)idx || in == (const void *)w) return PP_EINVAL;
+    if (sel_bias == w || (const void *)sel_bias == (const void *)idx) return PP_EINVAL;
     if (((uintptr_t)idx | (uintptr_t)w | (uintptr_t)sel_bias) & 3) return PP_EINVAL;
     if (flags & ~kRuleFlags) return PP_EINVAL;
     if (!(fabsf(scale) <= kFltMax)) return PP_EINVAL;  // also rejects NaN
@@ -1229,10 +1233,13 @@ extern "C" pp_status prunepath_route_topk(pp_layer *L, const uint16_t *x, int32_
                                           uint32_t flags, int32_t *expert_idx, float *gate_w,
                                           float *logits, void *hip_stream) {
     if (!L || !x || T < 1 || T > L->max_tokens) return PP_EINVAL;
-    if ((uintptr_t)logits & 3) return PP_EINVAL;
+    if (((uintptr_t)logits & 3) ||
+        (logits && (logits == gate_w || logits == sel_bias || (const void *)logits == (const void *)x ||
+                    (const void *)logits == (const void *)expert_idx)))
+        return PP_EINVAL;
     const int E = L->dm.E;
     const pp_status st =
-        check_rule(E, k, n_groups, top_groups, sel_bias, scale, flags, expert_idx, gate_w);
+        check_rule(x, E, k, n_groups, top_groups, sel_bias, scale, flags, expert_idx, gate_w);
     if (st != PP_OK) return st;
     hipStream_t s = static_cast<hipStream_t>(hip_stream);
     // the partial logits of the handle's router, in its scratch
@@ -1256,7 +1263,7 @@ extern "C" pp_status prunepath_route_topk_logits(const float *g, int32_t T, int3
     if (!g || ((uintptr_t)g & 3) || T < 1 || T > kMaxTopkRows || E < 1 || E > kMaxExperts)
         return PP_EINVAL;
     const pp_status st =
-        check_rule(E, k, n_groups, top_groups, sel_bias, scale, flags, expert_idx, gate_w);
+        check_rule(g, E, k, n_groups, top_groups, sel_bias, scale, flags, expert_idx, gate_w);
     if (st != PP_OK) return st;
     const TopkParams P = {{g, nullptr, nullptr, nullptr, nullptr, 0}, T, E, k, n_groups, top_groups,
                           sel_bias, scale, flags, expert_idx, gate_w, 0, 0, 0, 0, 0, 0, 0, 0, 0};

@@ -1,0 +1,34 @@
+"""Arrays of the routing calls that are the same: refused before any HIP call (runs without a GPU
+but for the call on a handle)."""
+import pytest
+
+import paper_2605_28283_amd as pp
+
+
+@pytest.mark.parametrize("g,bias,idx,w", [(16, 32, 16, 64), (16, 32, 48, 16), (16, 32, 32, 64),
+                                          (16, 32, 48, 32), (16, None, 48, 48)])
+def test_route_topk_logits_refuses_shared_arrays(g, bias, idx, w):
+    assert pp.load().prunepath_route_topk_logits(g, 8, 64, 4, 8, 4, bias, 1.0, 0, idx, w,
+                                                 None) == pp.PP_EINVAL
+
+
+@pytest.mark.gpu
+def test_handle_call_refuses_shared_arrays():
+    import torch
+    d, E = 64, 2
+    z = lambda *s: torch.zeros(s, dtype=torch.bfloat16, device="cuda")  # noqa: E731
+    h = pp.prunepath_create(d, 128 * E, E, 4, z(E, d), z(128 * E, d), z(128 * E, d), z(d, 128 * E))
+    try:
+        own = [torch.zeros(256, device="cuda") for _ in range(5)]
+        x, bias, idx, w, g = (a.data_ptr() for a in own)
+        f = lambda x, bias, idx, w, g: pp.load().prunepath_route_topk(  # noqa: E731
+            h, x, 4, None, 2, 1, 1, bias, 1.0, 0, idx, w, g, None)
+        for bad in ((x, bias, x, w, g), (x, bias, idx, x, g), (x, bias, idx, w, x),
+                    (x, bias, bias, w, g), (x, bias, idx, bias, g), (x, bias, idx, w, bias),
+                    (x, bias, idx, w, idx), (x, bias, idx, w, w)):
+            assert f(*bad) == pp.PP_EINVAL
+        assert f(x, bias, idx, w, g) == pp.PP_OK
+        assert f(x, None, idx, w, None) == pp.PP_OK
+        torch.cuda.synchronize()
+    finally:
+        pp.prunepath_destroy(h)
