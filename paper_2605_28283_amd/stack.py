@@ -23,10 +23,10 @@ from . import _lib as pp
 
 
 class DecodeStack:
-    """norms: one (weight, bias) pair of [d] fp32 tensors (or None) per layer, or None
-    for RMSNorm.  topk: a dict of prunepath_route_topk's k and, unless the defaults do,
-    n_groups, top_groups, scale, flags, and sel_bias, a list of one [E] fp32 tensor (or
-    None) per layer; tau is not used then."""
+    """norms: one pair (weight, bias) per layer, each a [d] fp32 tensor or None (1 and 0),
+    or None for RMSNorm.  topk: a dict of prunepath_route_topk's k and, unless the defaults
+    do, n_groups, top_groups, scale, flags, and sel_bias, a list of one [E] fp32 tensor (or
+    None) per layer, or None for no biases; tau is not used then."""
 
     def __init__(self, handles, d, E, T, tau, eps=1e-5, norms=None, topk=None):
         self.handles = list(handles)
@@ -35,6 +35,11 @@ class DecodeStack:
         self.norms = None if norms is None else list(norms)
         if self.norms is not None and len(self.norms) != self.L:
             raise ValueError("norms: %d pairs for %d layers" % (len(self.norms), self.L))
+        for n in self.norms or ():
+            if n is None or len(n) != 2:
+                raise ValueError("norms: a layer's entry that is not a pair (weight, bias)")
+            if any(a is not None and a.numel() != d for a in n):
+                raise ValueError("norms: a weight or bias that is not [%d]" % d)
         self.topk = None
         if topk is not None:
             self.topk = dict(n_groups=1, top_groups=1, scale=1.0, flags=0,
@@ -43,6 +48,8 @@ class DecodeStack:
             if unknown or "k" not in topk:
                 raise ValueError("topk: %s" % (sorted(unknown) or "no k"))
             self.topk.update(topk)
+            if self.topk["sel_bias"] is None:
+                self.topk["sel_bias"] = [None] * self.L
             if len(self.topk["sel_bias"]) != self.L:
                 raise ValueError("topk: %d selection biases for %d layers"
                                  % (len(self.topk["sel_bias"]), self.L))
