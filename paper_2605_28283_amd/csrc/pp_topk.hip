@@ -187,7 +187,7 @@ __device__ __forceinline__ double sigmoid64(float z) {
     return z >= 0.0f ? r : e * r;
 }
 // A score and c in 64 bits, each step rounded (no product is fused into a sum),
-// from 1 / (sum of e^(z - zmax)) added up by expert (exact_softmax_scale):
+// from 1 / (sum of e^(z - zmax)) in the order of exact_softmax_scale:
 // the same bits wherever they are formed, so that c's next to each other are
 // in one order in every kernel.
 __device__ __forceinline__ double score64(bool sig, float z, float zmax, double scale) {
@@ -315,15 +315,19 @@ __device__ __forceinline__ int groups_in_front(const TopkParams &P, double a, do
     return front;
 }
 
-// 1 / (sum of e^(z - zmax)) of a row in 64 bits, by the whole wavefront: lane l
-// adds those of experts l, l + 64, ..., then pairs of lanes.
+// 1 / (sum of e^(z - zmax)) of a row in 64 bits, by the whole wavefront, in the
+// order of route_topk_wide_k: groups spread over the lanes as for
+// groups_in_front, a lane's values, then pairs of lanes.
 __device__ __forceinline__ double exact_softmax_scale(const TopkParams &P, const float *zr,
                                                       float zmax, int lane) {
+    const int wl = P.lanes_log + 2, grp = lane >> wl;
     double S = 0.0;
+    if (grp < P.n_groups) {
 #pragma unroll 1
-    for (int e = lane; e < P.E; e += 64) {
-        const float z = zr[topk_place(P, e)];
-        if (z > -INFINITY) S += exp_neg((double)z - (double)zmax);
+        for (int i = lane & ((1 << wl) - 1); i < P.Gs; i += 1 << wl) {
+            const float z = zr[grp * P.Gp + i];
+            if (z > -INFINITY) S += exp_neg((double)z - (double)zmax);
+        }
     }
     S = wave_reduce(S, lane, [](double a, double b) { return a + b; });
     return S > 0.0 ? rcp64(S) : 0.0;
@@ -379,21 +383,15 @@ __device__ __forceinline__ void choose_row(const TopkParams &P, const float *zr,
     constexpr int NE = kMaxExperts / 64;
     const bool sig = (P.flags & PP_SCORE_SIGMOID) != 0;
     const bool top2 = (P.flags & PP_GROUP_TOP2) != 0;
-    double c[NE], s[NE], S = 0.0;
+    const double scale = sig ? 1.0 : exact_softmax_scale(P, zr, zmax, lane);
+    double c[NE], s[NE];
 #pragma unroll
     for (int q = 0; q < NE; ++q) {
         const int e = lane + 64 * q;
         const float z = e < P.E ? zr[topk_place(P, e)] : -INFINITY;
         c[q] = (double)z;
         s[q] = 0.0;
-        if (z > -INFINITY) s[q] = sig ? sigmoid64(z) : exp_neg((double)z - (double)zmax);
-        S += s[q];
-    }
-    if (!sig) {
-        S = wave_reduce(S, lane, [](double a, double b) { return a + b; });
-        const double r = S > 0.0 ? rcp64(S) : 0.0;
-#pragma unroll
-        for (int q = 0; q < NE; ++q) s[q] *= r;  // as in score64
+        if (z > -INFINITY) s[q] = score64(sig, z, zmax, scale);
     }
 #pragma unroll
     for (int q = 0; q < NE; ++q) {
@@ -860,17 +858,6 @@ __global__ __launch_bounds__(64 * kTopkWaves) void route_topk_wide_k(TopkParams 
                 by[q] = z[q] >= 0.0f ? d : by[q] * d;
             }
         } else {
-            if (P.n_groups > 1) {  // added up by expert (in one group S has that order)
-#pragma unroll
-                for (int q = 0; q < NQ; ++q)
-                    if (q << wl < held) cs[e0 + (q << wl)] = by[q];
-                wave_sync();
-                S = 0.0;
-#pragma unroll
-                for (int q = 0; q < kMaxExperts / 64; ++q)
-                    if (lane + 64 * q < E) S += cs[lane + 64 * q];
-                wave_sync();
-            }
             S = wave_reduce(S, lane, [](double a, double b) { return a + b; });
             const double r = S > 0.0 ? rcp64(S) : 0.0;
 #pragma unroll
@@ -927,6 +914,9 @@ __global__ __launch_bounds__(64 * kTopkWaves) void route_topk_wide_k(TopkParams 
     uint32_t last = kNone;
     bool close = false, unsure = false;
     int len = 0;
+    // A pass is short and its start is jumped to: near the end of a cache line
+    // it costs 20 ns more (k 32: 10.7 against 9.8 us).
+    asm volatile(".p2align 6");
 #pragma unroll 1
     for (int j = 0; j < k; ++j) {
         const bool over = j > 0 && last == kNone;
