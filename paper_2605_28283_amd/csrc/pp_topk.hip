@@ -1118,18 +1118,25 @@ void launch_topk_grad_nq(const TopkGradParams &P, hipStream_t s) {
         hipLaunchKernelGGL((route_topk_grad_k<NQ, true>), grid, block, 0, s, P);
 }
 
+// The builds by how many columns a lane has: every number up to 8, then every
+// other one, so that at most one column of a lane is empty.
+struct TopkGradBuild {
+    int columns;
+    void (*launch)(const TopkGradParams &, hipStream_t);
+};
+template <int NQ>
+constexpr TopkGradBuild topk_grad_build() {
+    return {NQ, launch_topk_grad_nq<NQ>};
+}
+constexpr TopkGradBuild kTopkGradBuilds[] = {
+    topk_grad_build<1>(),  topk_grad_build<2>(),  topk_grad_build<3>(),  topk_grad_build<4>(),
+    topk_grad_build<5>(),  topk_grad_build<6>(),  topk_grad_build<7>(),  topk_grad_build<8>(),
+    topk_grad_build<10>(), topk_grad_build<12>(), topk_grad_build<14>(), topk_grad_build<16>()};
+
 void launch_topk_grad(const TopkGradParams &P, hipStream_t s) {
-    const int need = (P.E + 15) / 16;
-    if (need <= 2)
-        launch_topk_grad_nq<2>(P, s);
-    else if (need <= 4)
-        launch_topk_grad_nq<4>(P, s);
-    else if (need <= 7)
-        launch_topk_grad_nq<7>(P, s);
-    else if (need <= 10)
-        launch_topk_grad_nq<10>(P, s);
-    else
-        launch_topk_grad_nq<16>(P, s);
+    const TopkGradBuild *B = kTopkGradBuilds;
+    while (16 * B->columns < P.E) ++B;  // at most 16: 256 experts
+    B->launch(P, s);
 }
 
 constexpr uint32_t kRuleFlags = PP_SCORE_SIGMOID | PP_TOPK_RENORM | PP_GROUP_TOP2;
