@@ -191,6 +191,13 @@ pp_status prunepath_ffn_prefill(pp_layer *L, const uint16_t *x, int32_t T, float
  *                order of c, then -1 where fewer than k can be chosen
  *   gate_w     : [T, k] fp32, the weights of the same slots, 0 in empty ones
  * An output may alias no other array (PP_EINVAL where two are the same).
+ * gate_w is off by at most a relative (24 + |x|) 2^-23, x the argument of its
+ * exponential: z_e less the row's (renormalised: the chosen ones') largest z,
+ * or min(z_e, 0) (renormalised: less the largest such of the chosen ones);
+ * values below the smallest normal float may be 0.
+ * An expert that is to take no part has a logit or bias of -inf.  A large
+ * finite bias does it too, but makes the calls slow (up to seven times): c's
+ * that 32 bits of the largest bias cannot tell apart are compared in 64.
  * Results do not depend on T or on the other tokens.  Nothing is allocated
  * and nothing but the outputs (and the handle's router scratch) is written, so
  * the calls may be captured; those without a handle may run at the same time
@@ -236,6 +243,7 @@ pp_status prunepath_route_topk_logits(const float *g, int32_t T, int32_t E, int3
  *   dgate_w       : [T, k] fp32; entries of empty slots are not read as
  *                   numbers (they may be NaN)
  *   flags         : the forward call's, and PP_GRAD_ADD
+ * dg is off by at most 100 2^-23 |scale| max_j |a_j| of its row.
  * dg may alias no other array.  The selection bias gets no gradient. */
 pp_status prunepath_route_topk_grad(const float *g, int32_t T, int32_t E, int32_t k,
                                     const int32_t *expert_idx, const float *dgate_w, float scale,

@@ -20,14 +20,21 @@
 // too near each other (exact_groups), neighbours of the list too near each
 // other or to what was left out (the list, with all that may belong in it, is
 // sorted by exact c: sort_list), and rows where that is more than 64 entries
-// (choose_row).  So c is compared in 64 bits wherever it matters, and few
-// tokens pay for it.
-// Bound by vector instructions: 16384 tokens of 256 experts, 8 groups, k 8,
-// sigmoid plus a bias take 13.2 us (11.0 among captured calls) for 17.8 MB,
-// 1057 vector instructions a wavefront, of which the nine passes are a third;
-// every score in 64 bits took 28.8 us, an argmax over 64-bit values 50.7.
+// (choose_row).  So c is compared in 64 bits wherever it matters.  Few tokens
+// pay for it while the biases are of the scores' size: the error of every c is
+// taken from the largest |bias| of an expert that takes part, so a single
+// finite one of -1e4 or -1e9 (a mask; -inf costs nothing) makes more or all
+// rows open, 12.4 us below to 26 and 81.
+// Neither memory nor one unit bounds it: 16384 tokens of 256 experts, 8 groups,
+// k 8, sigmoid plus a bias take 13.4 us (12.4 among captured calls) for 17.8
+// MB.  1109 vector instructions a wavefront, of which the nine passes are a
+// third, issue for about 7.5 us; all wavefronts are resident at once and wait
+// for half of their cycles, in the loads, the LDS round trips and the exact
+// tails.  Every score in 64 bits took 28.8 us, an argmax over 64-bit values 50.7.
 // Weights are formed in fp32; renormalised ones from scores relative to the
 // largest chosen one, so a row of scores that all underflow still has them.
+// Relative error (24 + |x|) 2^-23 with x the argument of the weight's
+// exponential, of which 20 2^-23 are a plain softmax weight's sum (kSoftmaxErr).
 // Deterministic: no floating-point atomics; a token's result does not depend
 // on T.
 #include <type_traits>
@@ -978,6 +985,10 @@ struct TopkGradParams {
 //   sigmoid                 dg_e = scale s_e (1 - s_e) a_e
 //   renormalised softmax    dg_e = scale q_e (a_e - D)
 //   renormalised sigmoid    dg_e = scale q_e (1 - s_e) (a_e - D)
+// In fp32: with A = max |a_j|, a score is off by (24 + |x|) 2^-23 of itself,
+// at most 25 2^-23 (p |x| <= 1 / e), |a_e - D| is at most 2 A, and D is off by
+// (24 + 6 + 9) 2^-23 A (x averages to at most log 256 over the scores; a sum of
+// 256 terms): 100 2^-23 |scale| A with the last products.
 // Bound by memory (dg is written whole): 16384 x 112, k 16, plain softmax
 // 5.8 us for 22 MB; a wavefront a token with the slots in turn took 57.  A token takes 16 lanes: lane c has
 // slots c, c + 16, ... and columns c, c + 16, ... (NQ of them); the slots'
@@ -1159,7 +1170,9 @@ pp_status check_rule(const void *in, int32_t E, int32_t k, int32_t n_groups, int
     return PP_OK;
 }
 
-// The builds by how many values a lane holds: 16 for 256 experts in one group.
+// The builds by how many values a lane holds, every number up to 8 and then in
+// steps of a fifth to two fifths: 16 for 256 experts in one group, 28 for nine
+// groups of 28, the most there are.
 struct TopkBuild {
     int values;
     void (*scores)(TopkParams);
@@ -1181,10 +1194,17 @@ struct TopkWideBuild {
 constexpr TopkWideBuild kTopkWideBuilds[] = {{4, route_topk_wide_k<4>},
                                              {7, route_topk_wide_k<7>}};
 // Up to so many tokens take a wavefront each if 16 lanes would hold more than
-// 8 values each, which makes the passes long: 256 experts, k 8, 64 tokens 4.7
-// against 5.7 us with 16 lanes each, 1024 tokens 5.1 against 5.8, 4096 tokens
-// 6.9 against 6.0.  With fewer values the 16 lanes are no slower (112 experts,
-// 64 tokens: 4.5 against 4.2 us).
+// 8 values each, which makes the passes long.  256 experts, k 8, a wavefront
+// each against 16 lanes each, us:
+//                            64 tokens   1024 tokens   4096 tokens
+//   order of logits          5.1  5.1    5.2   5.2     7.1   5.4
+//   the same, k 32           8.8  9.0   10.3  10.9    15.4  12.1
+//   sigmoid + bias           6.0  6.3    6.3   7.1     9.6   7.5
+//   the same, 8 groups       7.0  6.7    7.3   7.0    10.9   7.9
+//   softmax + bias, groups   6.9  6.4    7.3   8.9    11.0   9.1
+// With fewer values the 16 lanes are faster for few tokens and near for 1024:
+// 128 experts 5.3  4.5 (order of logits, 64 tokens), 6.0  5.5 (sigmoid + bias),
+// 5.3  4.8 and 6.3  6.3 at 1024.
 constexpr int kWideTokens = 1024;
 
 hipError_t launch_topk(TopkParams P, hipStream_t s) {

@@ -166,3 +166,24 @@ def test_norm_takes_an_eps_up_to_the_largest_float():
     rstd = 1.0 / np.sqrt(FLT_MAX)
     assert (np.abs(st[:, 1].cpu().numpy() - rstd) <= 4 * STEP * rstd).all()
     assert bool((u.abs() <= 10 * rstd).all())
+
+
+@pytest.mark.parametrize("sigmoid", [False, True])
+@pytest.mark.parametrize("renorm", [False, True])
+@pytest.mark.parametrize("std", [0.1, 3.0, 40.0])
+def test_gradient_is_as_near_as_the_header_says(sigmoid, renorm, std):
+    """100 2^-23 |scale| max |a|, however far the logits lie apart."""
+    import torch
+    for T, E, k in ((40, 256, 8), (9, 112, 112), (4100, 24, 3)):
+        rng = np.random.default_rng(E + k)
+        g = (rng.standard_normal((T, E)) * std).astype(np.float32)
+        c = case(k, 1, 1, None, 1.5, sigmoid, renorm)
+        idx, _ = route(g, c)
+        dw = rng.standard_normal((T, k)).astype(np.float32)
+        dg = torch.zeros((T, E), device="cuda")
+        pp.prunepath_route_topk_grad(dev(g), T, E, k, dev(idx, np.int32), dev(dw), 1.5,
+                                     flags_of(c), dg)
+        ref = op.route_topk_grad(g, idx, dw, 1.5, sigmoid, renorm)
+        tol = 100 * STEP * 1.5 * np.abs(dw).max(1, keepdims=True)
+        assert (np.abs(dg.cpu().numpy() - ref) <= tol).all()
+        check_weights(g[:40], c)
