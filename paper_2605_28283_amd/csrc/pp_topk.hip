@@ -1250,9 +1250,12 @@ extern "C" pp_status prunepath_route_topk(pp_layer *L, const uint16_t *x, int32_
                                           uint32_t flags, int32_t *expert_idx, float *gate_w,
                                           float *logits, void *hip_stream) {
     if (!L || !x || T < 1 || T > L->max_tokens) return PP_EINVAL;
-    if (((uintptr_t)logits & 3) ||
-        (logits && (logits == gate_w || logits == sel_bias || (const void *)logits == (const void *)x ||
-                    (const void *)logits == (const void *)expert_idx)))
+    if ((uintptr_t)logits & 3) return PP_EINVAL;
+    const void *const outs[] = {expert_idx, gate_w, logits};
+    for (const void *o : outs)
+        if (o && o == (const void *)inv_temp) return PP_EINVAL;
+    if (logits && (logits == gate_w || logits == sel_bias || (const void *)logits == (const void *)x ||
+                   (const void *)logits == (const void *)expert_idx))
         return PP_EINVAL;
     const int E = L->dm.E;
     const pp_status st =

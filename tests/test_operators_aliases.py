@@ -32,3 +32,21 @@ def test_handle_call_refuses_shared_arrays():
         torch.cuda.synchronize()
     finally:
         pp.prunepath_destroy(h)
+
+
+@pytest.mark.gpu
+def test_handle_call_refuses_outputs_in_the_temperatures():
+    import torch
+    d, E = 64, 2
+    z = lambda *s: torch.zeros(s, dtype=torch.bfloat16, device="cuda")  # noqa: E731
+    h = pp.prunepath_create(d, 128 * E, E, 4, z(E, d), z(128 * E, d), z(128 * E, d), z(d, 128 * E))
+    try:
+        own = [torch.ones(256, device="cuda") for _ in range(5)]
+        x, it, idx, w, g = (a.data_ptr() for a in own)
+        f = lambda idx, w, g: pp.load().prunepath_route_topk(  # noqa: E731
+            h, x, 4, it, 2, 1, 1, None, 1.0, 0, idx, w, g, None)
+        assert f(it, w, g) == f(idx, it, g) == f(idx, w, it) == pp.PP_EINVAL
+        assert f(idx, w, g) == f(idx, w, None) == pp.PP_OK
+        torch.cuda.synchronize()
+    finally:
+        pp.prunepath_destroy(h)
