@@ -1250,7 +1250,7 @@ extern "C" pp_status prunepath_route_topk(pp_layer *L, const uint16_t *x, int32_
                                           uint32_t flags, int32_t *expert_idx, float *gate_w,
                                           float *logits, void *hip_stream) {
     if (!L || !x || T < 1 || T > L->max_tokens) return PP_EINVAL;
-    if ((uintptr_t)logits & 3) return PP_EINVAL;
+    if (((uintptr_t)logits | (uintptr_t)inv_temp) & 3) return PP_EINVAL;
     const void *const outs[] = {expert_idx, gate_w, logits};
     for (const void *o : outs)
         if (o && o == (const void *)inv_temp) return PP_EINVAL;

@@ -50,3 +50,22 @@ def test_handle_call_refuses_outputs_in_the_temperatures():
         torch.cuda.synchronize()
     finally:
         pp.prunepath_destroy(h)
+
+
+@pytest.mark.gpu
+def test_handle_call_refuses_misaligned_arrays():
+    """fp32 and int32 arrays lie on 4 bytes, the temperatures among them."""
+    import torch
+    d, E = 64, 2
+    z = lambda *s: torch.zeros(s, dtype=torch.bfloat16, device="cuda")  # noqa: E731
+    h = pp.prunepath_create(d, 128 * E, E, 4, z(E, d), z(128 * E, d), z(128 * E, d), z(d, 128 * E))
+    try:
+        own = [torch.ones(256, device="cuda") for _ in range(6)]
+        at = [a.data_ptr() for a in own]
+        for bad in (None, 1, 2, 3, 4, 5):
+            x, it, bias, idx, w, g = (p + (2 if i == bad else 0) for i, p in enumerate(at))
+            st = pp.load().prunepath_route_topk(h, x, 4, it, 2, 1, 1, bias, 1.0, 0, idx, w, g, None)
+            assert st == (pp.PP_OK if bad is None else pp.PP_EINVAL)
+        torch.cuda.synchronize()
+    finally:
+        pp.prunepath_destroy(h)
